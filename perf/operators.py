@@ -347,11 +347,7 @@ def _kept(s):
             s["rope"] = sp.Rope(case["rot"], THETA, interleaved=case["interleaved"], **more)
         if case["kind"] == "prefix":
             size = sp.santapp_prefix_decode_workspace_bytes(s["geom"], case["prefix"], case["cap"])
-        elif case["kind"] == "prompt":
-            size = sp.santapp_prompt_workspace_bytes(s["geom"], s["lens"], s["new"])
-        else:
-            size = 0
-        s["workspace"] = torch.empty(size, dtype=torch.uint8, device="cuda")
+            s["workspace"] = torch.empty(size, dtype=torch.uint8, device="cuda")
     return sp, s["geom"]
 
 
@@ -375,7 +371,7 @@ def _call(s):
                                              prefix_token=s["token"], cap=case["softcap"], slopes=s["slopes"], out=s["out"],
                                              workspace=s["workspace"])
     return sp.santapp_prompt_attn(geom, s["lens"], s["q"], s["k"], s["v"], new_len=s["new"], prefix_len=s["both"],
-                                  cap=case["softcap"], slopes=s["slopes"], out=s["out"], workspace=s["workspace"])
+                                  cap=case["softcap"], slopes=s["slopes"], out=s["out"])
 
 
 def run(state):
