@@ -5,7 +5,8 @@ merge) runs in the library's CUDA kernels. PyTorch is used for device memory and
 streams. There is no CPU fallback: if the library is missing or cannot be loaded
 the first call raises.
 
-The functions keep the names of the C entry points (include/santapp.h, include/santapp_latent.h).
+The functions keep the names of the C entry points (include/santapp.h, include/santapp_latent.h,
+include/santapp_serve.h).
 """
 import ctypes
 import functools
@@ -37,6 +38,8 @@ EXPORTS = [
     "santapp_kmeans_fit_workspace_bytes", "santapp_kmeans_fit",
     "santapp_latent_sizes", "santapp_latent_build_teams", "santapp_latent_decode_workspace_bytes",
     "santapp_latent_decode_attn", "santapp_latent_dense_workspace_bytes", "santapp_latent_dense_decode_attn",
+    "santapp_rope_frequencies", "santapp_rope_append", "santapp_rope_prompt", "santapp_suffix_fork",
+    "santapp_prefix_decode_workspace_bytes", "santapp_prefix_decode_attn", "santapp_prompt_attn",
 ]
 LATENT_DIM, LATENT_ROPE_DIM, LATENT_ROW = 512, 64, 576
 
@@ -94,6 +97,16 @@ class CLatentTeams(ctypes.Structure):
                 ("row_token", ctypes.c_void_p), ("seq_row_off", ctypes.c_void_p), ("seq_team_off", ctypes.c_void_p),
                 ("rep_abs_max", ctypes.c_void_p), ("rows_total", ctypes.c_int64), ("teams_total", ctypes.c_int64),
                 ("max_teams_per_seq", ctypes.c_int32), ("max_rows_per_seq", ctypes.c_int32)]
+
+
+class CRope(ctypes.Structure):
+    _fields_ = [("rot_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("amplitude", ctypes.c_double),
+                ("inv_freq", ctypes.c_double * 64)]
+
+
+class CAttnOpts(ctypes.Structure):
+    _fields_ = [("scale", ctypes.c_float), ("cap", ctypes.c_float), ("slopes", ctypes.c_void_p),
+                ("status", ctypes.c_void_p)]
 
 
 def load_library(path: Optional[str] = None):
@@ -170,6 +183,22 @@ def load_library(path: Optional[str] = None):
     L.santapp_latent_decode_attn.restype = ctypes.c_int
     L.santapp_latent_dense_decode_attn.argtypes = [LG, LT, vp, vp, vp, i32, f32, vp, vp, sz, vp]
     L.santapp_latent_dense_decode_attn.restype = ctypes.c_int
+    i64, f64 = ctypes.c_int64, ctypes.c_double
+    G, R, O = ctypes.POINTER(CGeom), ctypes.POINTER(CRope), ctypes.POINTER(CAttnOpts)
+    L.santapp_rope_frequencies.argtypes = [R, f64, f64, f64, f64, f64]
+    L.santapp_rope_frequencies.restype = ctypes.c_int
+    L.santapp_rope_append.argtypes = [G, R, vp, i64, vp, i64, vp, i64, vp, vp, vp, vp, vp, i32, vp, vp]
+    L.santapp_rope_append.restype = ctypes.c_int
+    L.santapp_rope_prompt.argtypes = [G, R, i64, vp, i64, vp, i64, vp, i64, vp, vp, vp, vp, vp, i64, vp]
+    L.santapp_rope_prompt.restype = ctypes.c_int
+    L.santapp_suffix_fork.argtypes = [G, vp, vp, vp, vp, i32, vp, vp]
+    L.santapp_suffix_fork.restype = ctypes.c_int
+    L.santapp_prefix_decode_workspace_bytes.argtypes = [G, i64, i32]
+    L.santapp_prefix_decode_workspace_bytes.restype = sz
+    L.santapp_prefix_decode_attn.argtypes = [G, vp, vp, i64, i64, vp, vp, vp, vp, vp, i32, O, vp, vp, sz, vp]
+    L.santapp_prefix_decode_attn.restype = ctypes.c_int
+    L.santapp_prompt_attn.argtypes = [G, ctypes.POINTER(i32), ctypes.POINTER(i32), ctypes.POINTER(i32), vp, vp, vp, O, vp, vp]
+    L.santapp_prompt_attn.restype = ctypes.c_int
     if path is None:
         _lib = L
     return L
@@ -574,6 +603,189 @@ def santapp_latent_dense_decode_attn(geom: LatentGeometry, teams: LatentTeams, q
     _check(L.santapp_latent_dense_decode_attn(geom.ref(), ctypes.byref(teams.c), _ptr(q), _ptr(suffix_rows),
                                               _ptr(suffix_len), cap, scale, _ptr(out), _ptr(workspace),
                                               workspace.numel(), _stream_ptr(stream)))
+    return out
+
+
+# ------------------------------------------------------------------------------------------------
+# Around the decode step (include/santapp_serve.h)
+# ------------------------------------------------------------------------------------------------
+def _refuse(why):
+    raise SantappError(SANTAPP_ERR_INVALID_ARG, why)
+
+
+def _expect(name, t, shape, dtype, dense=True):
+    """The address of a tensor of exactly this shape and type on the current device (None in `shape`: any size). Not
+    dense: the first dimension may have any stride."""
+    if not t.is_cuda or t.get_device() != torch._C._cuda_getDevice():
+        _refuse(f"{name} must be a CUDA tensor on the current device")
+    if t.dtype != dtype:
+        _refuse(f"{name} must be {dtype}")
+    if len(t.shape) != len(shape) or any(want is not None and have != want for have, want in zip(t.shape, shape)):
+        _refuse(f"{name} must have the shape {list(shape)}, not {list(t.shape)}")
+    if not (t.is_contiguous() if dense or t.shape[0] == 0 else t[0].is_contiguous()):
+        _refuse(f"{name} must be contiguous" + ("" if dense else " behind its first dimension"))
+    return t.data_ptr()
+
+
+def _expect_or_none(name, t, shape, dtype):
+    return None if t is None else _expect(name, t, shape, dtype)
+
+
+def _token_stride(t):
+    """Elements from token to token (of one token: what a dense tensor would have)."""
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
+
+
+class Rope:
+    """Rotary positions. factor > 1 scales the frequencies for long contexts: with original_len by their turns over the
+    trained length (`low`, `high`), without it all alike (santapp_rope_frequencies). `inv_freq` replaces them all."""
+
+    def __init__(self, rot_dim: int = 128, theta: float = 10000.0, interleaved: bool = False, factor: float = 1.0,
+                 low: float = 1.0, high: float = 4.0, original_len: float = 0.0, amplitude: float = 1.0, inv_freq=None):
+        self.c = CRope(rot_dim, 1 if interleaved else 0, amplitude)
+        if inv_freq is None:
+            _check(load_library().santapp_rope_frequencies(ctypes.byref(self.c), theta, factor, low, high, original_len))
+        else:
+            values = [float(x) for x in inv_freq]
+            if len(values) != rot_dim // 2 or rot_dim > 128:
+                _refuse("inv_freq holds rot_dim / 2 values")
+            self.c.inv_freq[:len(values)] = values
+
+    @property
+    def inv_freq(self):
+        return list(self.c.inv_freq[:self.c.rot_dim // 2])
+
+
+def _rope_rows(geom, n, q, k, v, q_out):
+    d, dt = geom.head_dim, geom.torch_dtype
+    if q_out is None:
+        q_out = torch.empty((n, geom.n_q_heads, d), dtype=dt, device=q.device)
+    return q_out, [_expect("q", q, (n, geom.n_q_heads, d), dt, False), _token_stride(q),
+                   _expect("k", k, (n, geom.n_kv_heads, d), dt, False), _token_stride(k),
+                   _expect("v", v, (n, geom.n_kv_heads, d), dt, False), _token_stride(v)], \
+        _expect("q_out", q_out, (n, geom.n_q_heads, d), dt)
+
+
+def santapp_rope_append(geom: Geometry, rope: Rope, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
+                        base_pos: torch.Tensor, suffix_len: torch.Tensor, k_suffix: torch.Tensor, v_suffix: torch.Tensor,
+                        q_out: Optional[torch.Tensor] = None, suffix_len_out: Optional[torch.Tensor] = None,
+                        stream=None) -> torch.Tensor:
+    """q [B, Hq, d], k and v [B, Hkv, d] (any stride between tokens); base_pos, suffix_len int32 [B]; k_suffix, v_suffix
+    [B, Hkv, cap, d]. Row suffix_len[b] is written, q_out returned; suffix_len_out (may be suffix_len) gets suffix_len + 1."""
+    L = load_library()
+    B = geom.n_seqs
+    q_out, rows, q_dst = _rope_rows(geom, B, q, k, v, q_out)
+    shape = (B, geom.n_kv_heads, None, geom.head_dim)
+    ks, vs = _expect("k_suffix", k_suffix, shape, geom.torch_dtype), _expect("v_suffix", v_suffix, tuple(k_suffix.shape), geom.torch_dtype)
+    _check(L.santapp_rope_append(geom.ref(), ctypes.byref(rope.c), *rows, _expect("base_pos", base_pos, (B,), torch.int32),
+                                 _expect("suffix_len", suffix_len, (B,), torch.int32), q_dst, ks, vs, k_suffix.shape[2],
+                                 _expect_or_none("suffix_len_out", suffix_len_out, (B,), torch.int32), _stream_ptr(stream)))
+    return q_out
+
+
+def santapp_rope_prompt(geom: Geometry, rope: Rope, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
+                        positions: Optional[torch.Tensor], k_prompt: torch.Tensor, v_prompt: torch.Tensor,
+                        dst_row: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
+                        stream=None) -> torch.Tensor:
+    """q [n, Hq, d], k and v [n, Hkv, d] (any stride between tokens); positions, dst_row int32 [n] or None (the row's
+    index); k_prompt, v_prompt [Hkv, rows, d], written at dst_row. Returns q_out [n, Hq, d]."""
+    L = load_library()
+    n = q.shape[0]
+    q_out, rows, q_dst = _rope_rows(geom, n, q, k, v, q_out)
+    shape = (geom.n_kv_heads, None, geom.head_dim)
+    kp, vp = _expect("k_prompt", k_prompt, shape, geom.torch_dtype), _expect("v_prompt", v_prompt, tuple(k_prompt.shape), geom.torch_dtype)
+    _check(L.santapp_rope_prompt(geom.ref(), ctypes.byref(rope.c), n, *rows,
+                                 _expect_or_none("positions", positions, (n,), torch.int32),
+                                 _expect_or_none("dst_row", dst_row, (n,), torch.int32), q_dst, kp, vp, k_prompt.shape[1],
+                                 _stream_ptr(stream)))
+    return q_out
+
+
+def santapp_suffix_fork(geom: Geometry, src: torch.Tensor, suffix_len: torch.Tensor, k_suffix: torch.Tensor,
+                        v_suffix: torch.Tensor, suffix_len_out: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Slot b of k_suffix / v_suffix [B, Hkv, cap, d] continues slot src[b] (int32 [B]; outside [0, B): freed), in place;
+    suffix_len_out (not suffix_len) gets the new lengths."""
+    L = load_library()
+    B = geom.n_seqs
+    shape = (B, geom.n_kv_heads, None, geom.head_dim)
+    ks, vs = _expect("k_suffix", k_suffix, shape, geom.torch_dtype), _expect("v_suffix", v_suffix, tuple(k_suffix.shape), geom.torch_dtype)
+    _check(L.santapp_suffix_fork(geom.ref(), _expect("src", src, (B,), torch.int32),
+                                 _expect("suffix_len", suffix_len, (B,), torch.int32), ks, vs, k_suffix.shape[2],
+                                 _expect_or_none("suffix_len_out", suffix_len_out, (B,), torch.int32), _stream_ptr(stream)))
+
+
+def santapp_prefix_decode_workspace_bytes(geom: Geometry, prefix_len: int, suffix_cap: int) -> int:
+    return int(load_library().santapp_prefix_decode_workspace_bytes(geom.ref(), prefix_len, suffix_cap))
+
+
+def _attn_opts(geom, scale, cap, slopes, status):
+    return CAttnOpts(scale, cap, _expect_or_none("slopes", slopes, (geom.n_q_heads,), torch.float32),
+                     _expect_or_none("status", status, (1,), torch.int32))
+
+
+def santapp_prefix_decode_attn(geom: Geometry, k_prefix: Optional[torch.Tensor], v_prefix: Optional[torch.Tensor],
+                               q: torch.Tensor, k_suffix: Optional[torch.Tensor], v_suffix: Optional[torch.Tensor],
+                               suffix_len: Optional[torch.Tensor], scale: float = 0.0, cap: float = 0.0,
+                               slopes: Optional[torch.Tensor] = None, prefix_token: Optional[torch.Tensor] = None,
+                               out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                               status: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """One prompt for the whole batch: k_prefix, v_prefix [Hkv, N, d] (the planes may lie further apart; None: no prompt),
+    prefix_token int32 of the same planes or None; q [B, Hq, d]; suffix as in santapp_decode_attn. fp32 [B, Hq, d]."""
+    L = load_library()
+    B, kv, d, dt = geom.n_seqs, geom.n_kv_heads, geom.head_dim, geom.torch_dtype
+    n = plane = 0
+    kp = vp = tok = None
+    if k_prefix is not None:
+        n = k_prefix.shape[1]
+        kp = _expect("k_prefix", k_prefix, (kv, None, d), dt, False)
+        vp = _expect("v_prefix", v_prefix, (kv, n, d), dt, False)
+        plane = k_prefix.stride(0) // d if kv > 1 else n
+        if kv > 1 and (k_prefix.stride(0) % d or v_prefix.stride(0) != k_prefix.stride(0)):
+            _refuse("the planes of k_prefix and v_prefix must lie whole rows and equally far apart")
+        if prefix_token is not None:
+            tok = _expect("prefix_token", prefix_token, (kv, n), torch.int32, False)
+            if kv > 1 and prefix_token.stride(0) != plane:
+                _refuse("the planes of prefix_token must lie as far apart as those of k_prefix")
+    ks = vs = None
+    suffix_cap = 0
+    if k_suffix is not None:
+        suffix_cap = k_suffix.shape[2]
+        ks = _expect("k_suffix", k_suffix, (B, kv, None, d), dt)
+        vs = _expect("v_suffix", v_suffix, (B, kv, suffix_cap, d), dt)
+    if out is None:
+        out = torch.empty((B, geom.n_q_heads, d), dtype=torch.float32, device=q.device)
+    if workspace is None:
+        workspace = torch.empty(santapp_prefix_decode_workspace_bytes(geom, n, suffix_cap), dtype=torch.uint8, device=q.device)
+    o = _attn_opts(geom, scale, cap, slopes, status)
+    _check(L.santapp_prefix_decode_attn(geom.ref(), kp, vp, n, plane, tok, _expect("q", q, (B, geom.n_q_heads, d), dt), ks, vs,
+                                        _expect_or_none("suffix_len", suffix_len, (B,), torch.int32), suffix_cap,
+                                        ctypes.byref(o), _expect("out", out, (B, geom.n_q_heads, d), torch.float32),
+                                        _expect("workspace", workspace, (None,), torch.uint8), workspace.numel(),
+                                        _stream_ptr(stream)))
+    return out
+
+
+def santapp_prompt_attn(geom: Geometry, prompt_len, q: torch.Tensor, k_prompt: torch.Tensor, v_prompt: torch.Tensor,
+                        new_len=None, prefix_len=None, scale: float = 0.0, cap: float = 0.0,
+                        slopes: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                        status: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """q [sum(new_len or prompt_len), Hq, d]: the last new_len rows of each sequence; k_prompt, v_prompt
+    [Hkv, sum(prompt_len), d]. Returns the element type, shaped like q."""
+    L = load_library()
+    if len(prompt_len) != geom.n_seqs or any(x is not None and len(x) != geom.n_seqs for x in (new_len, prefix_len)):
+        _refuse("prompt_len, new_len and prefix_len hold a length per sequence")
+    n, keys, d, dt = sum(prompt_len if new_len is None else new_len), sum(prompt_len), geom.head_dim, geom.torch_dtype
+    if out is None:
+        out = torch.empty((n, geom.n_q_heads, d), dtype=dt, device=q.device)
+    if n == 0:
+        return out
+    o = _attn_opts(geom, scale, cap, slopes, status)
+    _check(L.santapp_prompt_attn(geom.ref(), _i32_array(prompt_len), None if new_len is None else _i32_array(new_len),
+                                 None if prefix_len is None else _i32_array(prefix_len),
+                                 _expect("q", q, (n, geom.n_q_heads, d), dt),
+                                 _expect("k_prompt", k_prompt, (geom.n_kv_heads, keys, d), dt),
+                                 _expect("v_prompt", v_prompt, (geom.n_kv_heads, keys, d), dt), ctypes.byref(o),
+                                 _expect("out", out, (n, geom.n_q_heads, d), dt), _stream_ptr(stream)))
     return out
 
 

@@ -55,6 +55,15 @@ int check_geom(const santapp_geom *g)
     return SANTAPP_OK;
 }
 
+}  // namespace
+
+namespace santapp {
+int check_geometry(const santapp_geom *g) { return check_geom(g); }
+void begin_call() { g_cuda_error[0] = 0; g_launches = 0; }
+}  // namespace santapp
+
+namespace {
+
 int teams_in_sequence(int N, int P, int R)
 {
     const int full = N / P, tail = N % P;

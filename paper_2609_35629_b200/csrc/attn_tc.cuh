@@ -1,0 +1,492 @@
+// Attention of many query rows over the rows of one KV head, on the fifth-generation tensor cores: the part that
+// santapp_prefix_decode_attn (prefix.cu) and santapp_prompt_attn (prompt.cu) share.
+//
+// The query heads of a KV head are rows of one matrix (row t * G + g: head g of token t), so keys and values are
+// fetched once for the whole group. A block works on two accumulators ("streams") of 128 query rows; keys come in
+// tiles of 128:
+//   S = Q K^T        128 x 128 x 128, both operands in shared memory (128-byte swizzle, as TMA leaves them)
+//   P = exp2(S ...)  a thread per row: tcgen05.ld of its 128 scores, running maximum and sum in fp32, weights
+//                    written back over the scores as 16-bit values (tensor memory)
+//   O += P V         P from tensor memory, V as it lies in memory (N-major)
+// While the tensor core does stream 0's O += P V and its next S, the other stream's warps take their exponentials.
+// With more than 128 query rows the streams are two row tiles over the same keys (a tile of keys is fetched
+// once for both); with fewer they take the key tiles of the same rows in turn and are joined at the end.
+//
+// Weights: kTwo splits a weight into two 16-bit terms, p = hi + lo (off by at most 2^-16 of it, bf16), two products with V:
+// outputs good to fp32. Without, a weight is rounded once (2^-8, bf16), for outputs that are 16 bits wide anyway.
+// The running maximum is renewed only when a score passes it by 2^kSlack: until then weights are at most 2^kSlack, and O need
+// not be scaled; statistics and sums are fp32. fp16 weights carry a factor 2^7 (at most 2^15; the smallest kept is 2^-31 of one), which
+// cancels in O / l.
+//
+// Every wait is bounded: one that runs out makes all roles of the block stop, waits for its own copies and products, and the
+// results are NaN (and bit 2 of the status word).
+#pragma once
+#include <cuda.h>
+#include <math_constants.h>
+
+#include "common.cuh"
+#include "santapp_serve.h"
+#include "tc.cuh"
+
+namespace santapp {
+
+constexpr int kTaThreads = 320;           // warps 0-3, 4-7: a row each of streams 0, 1; warp 8: copies; warp 9: products
+constexpr int kTaTile = 128;              // query rows of a stream, keys of a tile
+constexpr int kTaTileBytes = kTaTile * kHeadDim * 2;
+constexpr int kTaRing = 5;                // tiles of keys or values under way
+constexpr float kTaSlack = 8.f;
+
+struct TaSmem {
+    alignas(1024) unsigned char q[2][kTaTileBytes];
+    unsigned char ring[kTaRing][kTaTileBytes];
+    uint64_t full[kTaRing], empty[kTaRing];   // a tile has landed; the products have left it
+    uint64_t q_ready, s_ready[2], p_ready[2], done[2];
+    uint64_t pos_ready[2][2];
+    alignas(16) float pos[2][2][kTaTile];                 // positions of the keys of a stream's tile, less n_keys; by tile parity
+    uint32_t tmem;
+    int failed;
+};
+constexpr int kTaSmemBytes = sizeof(TaSmem);
+static_assert(kTaSmemBytes <= 227 * 1024, "shared memory budget");
+
+// What a block works on.
+struct TaItem {
+    int head0;                // first query head of the KV head
+    int group, n_q;
+    const uint16_t *q;        // row r is q + ((r / group) * n_q + head0 + r % group) * 128
+    int n_rows;               // query rows from r = row0 on that are real
+    int row0;
+    int plane;                // KV head: the third coordinate of the planes
+    int key0;                 // plane row of key 0
+    int n_keys;               // rows behind this belong to somebody else
+    int tile0;                // first key tile
+    int count[2];             // key tiles of each stream
+    bool shared;              // the streams are two row tiles over the same keys
+    bool fix_tail;            // the planes hold rows behind n_keys: they are zeroed in V's last tile (0 times NaN is no 0)
+};
+struct TaScore {
+    float scale_log2;         // scale * log2 e
+    float cap_in, cap_log2;   // scale / cap, cap * log2 e
+    const float *slopes;
+    int32_t *status;
+};
+
+__device__ __forceinline__ uint32_t ta_addr(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ int ta_byte(int r, int ch)   // 16-byte piece ch of row r: two blocks of 64 values, pieces XOR-swizzled
+{
+    return (ch >> 3) * (kTaTile * 128) + r * 128 + (((ch & 7) ^ (r & 7)) << 4);
+}
+__device__ __forceinline__ float ta_ex2(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+template <bool kHalf>
+__device__ __forceinline__ uint32_t ta_pack(float lo, float hi)
+{
+    uint32_t r;
+    if constexpr (kHalf) asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    else                 asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+// A operand in tensor memory
+__device__ __forceinline__ void ta_mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate)
+{
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+                 "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}\n" ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate)
+                 : "memory");
+}
+// 32 columns, on their way until ta_ld_wait
+__device__ __forceinline__ void ta_ld32(uint32_t taddr, float *v)
+{
+    uint32_t *u = reinterpret_cast<uint32_t *>(v);
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+                 "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+                 : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]), "=r"(u[4]), "=r"(u[5]), "=r"(u[6]), "=r"(u[7]), "=r"(u[8]),
+                   "=r"(u[9]), "=r"(u[10]), "=r"(u[11]), "=r"(u[12]), "=r"(u[13]), "=r"(u[14]), "=r"(u[15]), "=r"(u[16]), "=r"(u[17]),
+                   "=r"(u[18]), "=r"(u[19]), "=r"(u[20]), "=r"(u[21]), "=r"(u[22]), "=r"(u[23]), "=r"(u[24]), "=r"(u[25]), "=r"(u[26]),
+                   "=r"(u[27]), "=r"(u[28]), "=r"(u[29]), "=r"(u[30]), "=r"(u[31])
+                 : "r"(taddr));
+}
+__device__ __forceinline__ void ta_tie(float *v)         // nothing computed from these 32 values moves ahead of this point
+{
+    uint32_t *u = reinterpret_cast<uint32_t *>(v);
+    asm volatile("" : "+r"(u[0]), "+r"(u[1]), "+r"(u[2]), "+r"(u[3]), "+r"(u[4]), "+r"(u[5]), "+r"(u[6]), "+r"(u[7]), "+r"(u[8]),
+                      "+r"(u[9]), "+r"(u[10]), "+r"(u[11]), "+r"(u[12]), "+r"(u[13]), "+r"(u[14]), "+r"(u[15]), "+r"(u[16]), "+r"(u[17]),
+                      "+r"(u[18]), "+r"(u[19]), "+r"(u[20]), "+r"(u[21]), "+r"(u[22]), "+r"(u[23]), "+r"(u[24]), "+r"(u[25]), "+r"(u[26]),
+                      "+r"(u[27]), "+r"(u[28]), "+r"(u[29]), "+r"(u[30]), "+r"(u[31]));
+}
+__device__ __forceinline__ void ta_ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void ta_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void ta_st16(uint32_t taddr, const uint32_t *v)
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};"
+                 :: "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]),
+                   "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]), "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void ta_st32(uint32_t taddr, const float *f)
+{
+    const uint32_t *v = reinterpret_cast<const uint32_t *>(f);
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+                 "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31};"
+                 :: "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]),
+                   "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]), "r"(v[16]), "r"(v[17]),
+                   "r"(v[18]), "r"(v[19]), "r"(v[20]), "r"(v[21]), "r"(v[22]), "r"(v[23]), "r"(v[24]), "r"(v[25]), "r"(v[26]),
+                   "r"(v[27]), "r"(v[28]), "r"(v[29]), "r"(v[30]), "r"(v[31]), "r"(taddr) : "memory");
+}
+// 64 values (128 bytes) x 128 rows of plane `z` from row y on
+__device__ __forceinline__ void ta_copy(uint32_t dst, const CUtensorMap *map, int x, int y, int z, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.tensor.3d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+                 ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void ta_named_barrier(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
+
+// A wait returns false once any of the block's waits has run out.
+__device__ __forceinline__ bool ta_wait(TaSmem &sm, uint64_t *bar, uint32_t parity)
+{
+    if (*reinterpret_cast<volatile int *>(&sm.failed)) return false;
+    if (tc_wait(ta_addr(bar), parity)) return true;
+    *reinterpret_cast<volatile int *>(&sm.failed) = 1;
+    return false;
+}
+// The same for a whole warp, whose lanes agree on the answer.
+__device__ __forceinline__ bool ta_wait_warp(TaSmem &sm, uint64_t *bar, uint32_t parity)
+{
+    return __all_sync(0xFFFFFFFFu, ta_wait(sm, bar, parity));
+}
+
+// The order in which key and value tiles are first used, the same for the warp that copies and the one that issues products.
+// use(value?, tile, stream, c): stream's c-th tile as keys (false) or values (true).
+template <typename Use>
+__device__ __forceinline__ void ta_order(const TaItem &it, Use use)
+{
+    const int most = max(it.count[0], it.count[1]);
+    for (int s = 0; s < 2; ++s)
+        if (it.count[s] > 0)
+            if (!use(false, s, 0)) return;
+    for (int c = 0; c < most; ++c)
+        for (int s = 0; s < 2; ++s) {
+            if (c >= it.count[s]) continue;
+            if (!use(true, s, c)) return;
+            if (c + 1 < it.count[s])
+                if (!use(false, s, c + 1)) return;
+        }
+}
+
+// One stream's rows: thread t of 128 owns row t. `vis`: keys [0, vis) are seen by the row; q_pos its position; key_pos
+// the positions of the plane's keys (null: their index). Leaves the statistics (maximum in log2 units, sum).
+template <bool kHalf, bool kTwo, bool kCap, bool kBias>
+__device__ __forceinline__ bool ta_softmax(TaSmem &sm, const TaItem &it, const TaScore &sc, int s, bool live, int vis, int q_pos,
+                                           float slope_log2, const int32_t *key_pos, float &m, float &l)
+{
+    constexpr float kShift = kHalf ? 7.f : 0.f;
+    const int t = threadIdx.x & 127;
+    const uint32_t lanes = (uint32_t)((threadIdx.x >> 5) & 3) << 21;
+    const uint32_t t_s = sm.tmem + lanes + 128u * s, t_o = sm.tmem + lanes + 256u + 128u * s;
+    const bool warp_live = __any_sync(0xFFFFFFFFu, live);
+    m = -CUDART_INF_F;
+    l = 0.f;
+    for (int c = 0; c < it.count[s]; ++c) {
+        const int tile = it.tile0 + (it.shared ? c : 2 * c + s), kb = tile * kTaTile;
+        if (kBias && key_pos != nullptr) {
+            // (relative to n_keys, so that near keys of a very long prompt keep whole distances in fp32; who writes here has
+            // seen all 128 threads at the tile before this one, that is behind the reading of the tile before that)
+            sm.pos[s][c & 1][t] = kb + t < it.n_keys ? (float)(key_pos[kb + t] - it.n_keys) : 0.f;
+            mbar_arrive(ta_addr(&sm.pos_ready[s][c & 1]));
+            if (!ta_wait_warp(sm, &sm.pos_ready[s][c & 1], (uint32_t)(c >> 1) & 1u)) return false;
+        }
+        if (!ta_wait_warp(sm, &sm.s_ready[s], c & 1)) return false;
+        if (warp_live) {
+            tc_fence_after();
+            float v[kTaTile];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) ta_ld32(t_s + 32 * q, v + 32 * q);
+            ta_ld_wait();
+#pragma unroll
+            for (int q = 0; q < 4; ++q) ta_tie(v + 32 * q);
+            if constexpr (kCap) {
+                // tanh from e = exp(-2 |x|): (1 - e) / (1 + e), sign of x
+#pragma unroll
+                for (int i = 0; i < kTaTile; ++i) {
+                    const float x = v[i] * sc.cap_in;
+                    const float e = ta_ex2(-2.885390082f * fabsf(x));
+                    v[i] = copysignf(__fdividef(1.f - e, 1.f + e), x) * sc.cap_log2;
+                }
+            } else if constexpr (kBias) {
+#pragma unroll
+                for (int i = 0; i < kTaTile; ++i) v[i] *= sc.scale_log2;
+            }
+            if constexpr (kBias) {
+                if (key_pos != nullptr) {
+                    const float d = (float)(q_pos - it.n_keys);
+#pragma unroll
+                    for (int i = 0; i < kTaTile; i += 4) {
+                        const float4 p = *reinterpret_cast<const float4 *>(&sm.pos[s][c & 1][i]);
+                        v[i] = fmaf(-slope_log2, fabsf(d - p.x), v[i]);
+                        v[i + 1] = fmaf(-slope_log2, fabsf(d - p.y), v[i + 1]);
+                        v[i + 2] = fmaf(-slope_log2, fabsf(d - p.z), v[i + 2]);
+                        v[i + 3] = fmaf(-slope_log2, fabsf(d - p.w), v[i + 3]);
+                    }
+                } else {
+                    const float d = (float)(q_pos - kb);
+#pragma unroll
+                    for (int i = 0; i < kTaTile; ++i) v[i] = fmaf(-slope_log2, fabsf(d - (float)i), v[i]);
+                }
+            }
+            const int seen = vis - kb;
+            if (__any_sync(0xFFFFFFFFu, seen < kTaTile)) {
+#pragma unroll
+                for (int i = 0; i < kTaTile; ++i) v[i] = i < seen ? v[i] : -CUDART_INF_F;
+            }
+            float mx = v[0];
+#pragma unroll
+            for (int i = 1; i < kTaTile; ++i) mx = fmaxf(mx, v[i]);
+            constexpr bool kRaw = !kCap && !kBias;          // v is in units of the product, not yet scaled
+            if constexpr (kRaw) mx *= sc.scale_log2;
+            const float m_new = fmaxf(m, mx);
+            if (c == 0) {
+                m = m_new;
+            } else if (__any_sync(0xFFFFFFFFu, m_new > m + kTaSlack)) {
+                const float f = m_new == -CUDART_INF_F ? 1.f : ta_ex2(m - m_new);
+                float o[32];
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    ta_ld32(t_o + 32 * q, o);
+                    ta_ld_wait();
+                    ta_tie(o);
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) o[i] *= f;
+                    ta_st32(t_o + 32 * q, o);
+                }
+                l *= f;
+                m = m_new;
+            }
+            const float shift = kShift - (m == -CUDART_INF_F ? 0.f : m), mul = kRaw ? sc.scale_log2 : 1.f;
+            float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                uint32_t hi[16], lo[16];
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const float p0 = ta_ex2(fmaf(v[32 * q + 2 * i], mul, shift)), p1 = ta_ex2(fmaf(v[32 * q + 2 * i + 1], mul, shift));
+                    sum[(2 * i) & 3] += p0;
+                    sum[(2 * i + 1) & 3] += p1;
+                    hi[i] = ta_pack<kHalf>(p0, p1);
+                    if constexpr (kTwo) lo[i] = ta_pack<kHalf>(p0 - elem_lo<kHalf>(hi[i]), p1 - elem_hi<kHalf>(hi[i]));
+                }
+                ta_st16(t_s + 16 * q, hi);
+                if constexpr (kTwo) ta_st16(t_s + 64 + 16 * q, lo);
+            }
+            l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+            ta_st_wait();
+            tc_fence_before();
+        }
+        mbar_arrive(ta_addr(&sm.p_ready[s]));
+    }
+    m -= kShift;                                           // the factor of the weights is the sum's too
+    if (it.count[s] > 0) {
+        if (!ta_wait_warp(sm, &sm.done[s], 0)) return false;
+        tc_fence_after();
+    }
+    return true;
+}
+
+// The block: set-up, copies, products. `rows(row, vis, q_pos)` tells how many keys a row sees and its position; `finish(ok, s, r, live, m, l)`
+// gets the statistics of stream s's row r of the item and takes O out of tensor memory (ta_rows).
+template <bool kHalf, bool kTwo, bool kCap, bool kBias, typename Rows, typename Finish>
+__device__ __forceinline__ void ta_block(TaSmem &sm, const TaItem &it, const TaScore &sc, const CUtensorMap *k_map, const CUtensorMap *v_map,
+                                         const int32_t *key_pos, Rows rows, Finish finish)
+{
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    if (tid == 0) {
+        sm.failed = 0;
+        for (int i = 0; i < kTaRing; ++i) {
+            asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(ta_addr(&sm.full[i])), "r"(1));
+            asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(ta_addr(&sm.empty[i])), "r"(1));
+        }
+        asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(ta_addr(&sm.q_ready)), "r"(256));
+        for (int s = 0; s < 2; ++s) {
+            asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(ta_addr(&sm.s_ready[s])), "r"(1));
+            asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(ta_addr(&sm.p_ready[s])), "r"(128));
+            asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(ta_addr(&sm.done[s])), "r"(1));
+            for (int i = 0; i < 2; ++i) asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(ta_addr(&sm.pos_ready[s][i])), "r"(128));
+        }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 9) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(ta_addr(&sm.tmem)), "r"(512) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::);
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+
+    if (warp < 8) {
+        // ---- the queries, then a row of scores per thread ----
+        const int tiles = it.shared ? 2 : 1;
+        for (int e = tid; e < tiles * kTaTile * 16; e += 256) {
+            const int r = e >> 4, ch = e & 15, row = it.row0 + r;
+            uint4 x = make_uint4(0, 0, 0, 0);
+            if (r < it.n_rows) x = reinterpret_cast<const uint4 *>(it.q + ((int64_t)(row / it.group) * it.n_q + it.head0 + row % it.group) * kHeadDim)[ch];
+            *reinterpret_cast<uint4 *>(sm.q[r >> 7] + ta_byte(r & 127, ch)) = x;
+        }
+        proxy_fence();
+        mbar_arrive(ta_addr(&sm.q_ready));
+        const int s = warp >> 2, r = (tid & 127) + (it.shared ? kTaTile * s : 0);
+        bool live = r < it.n_rows;
+        int vis = it.n_keys;
+        int q_pos = 0;
+        float slope = 0.f, m, l;
+        if (live) rows(it.row0 + r, vis, q_pos);
+        if (kBias && live) slope = 1.4426950409f * sc.slopes[it.head0 + (it.row0 + r) % it.group];
+        const bool ok = ta_softmax<kHalf, kTwo, kCap, kBias>(sm, it, sc, s, live, vis, q_pos, slope, key_pos, m, l);
+        finish(ok, s, r, live, m, l);
+    } else if (warp == 8) {
+        // ---- copies: tiles in the order of their first use ----
+        if (lane == 0) {
+            int n = 0;                                     // tiles asked for
+            bool ok = true;
+            ta_order(it, [&](bool value, int s, int c) {
+                if (it.shared && s == 1 && c < it.count[0]) return true;       // stream 0 has asked for it
+                const int slot = n % kTaRing;
+                if (n >= kTaRing && !ta_wait(sm, &sm.empty[slot], (uint32_t)(n / kTaRing - 1) & 1u)) return ok = false;
+                const uint32_t bar = ta_addr(&sm.full[slot]), dst = ta_addr(sm.ring[slot]);
+                const int tile = it.tile0 + (it.shared ? c : 2 * c + s);
+                asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(kTaTileBytes) : "memory");
+                const CUtensorMap *map = value ? v_map : k_map;
+                ta_copy(dst, map, 0, it.key0 + tile * kTaTile, it.plane, bar);
+                ta_copy(dst + kTaTileBytes / 2, map, 64, it.key0 + tile * kTaTile, it.plane, bar);
+                ++n;
+                return true;
+            });
+            // nothing leaves while a copy is under way (in the normal course the products have waited for all of them)
+            for (int i = max(0, n - kTaRing); i < n; ++i) tc_wait(ta_addr(&sm.full[i % kTaRing]), (uint32_t)(i / kTaRing) & 1u);
+        }
+    } else {
+        // ---- products ----
+        const uint32_t idesc_s = tc_idesc(kTaTile, kTaTile, 0, 0, kHalf), idesc_o = tc_idesc(kTaTile, kHeadDim, 0, 1, kHalf);
+        int n = 0, k_slot = 0, v_slot = 0;
+        bool ok = ta_wait_warp(sm, &sm.q_ready, 0);
+        if (ok)
+            ta_order(it, [&](bool value, int s, int c) {
+                int &slot = value ? v_slot : k_slot;
+                const int tile = it.tile0 + (it.shared ? c : 2 * c + s);
+                const bool first = !(it.shared && s == 1 && c < it.count[0]), last = !(it.shared && s == 0 && c < it.count[1]);
+                if (first) {
+                    slot = n % kTaRing;
+                    if (!ta_wait_warp(sm, &sm.full[slot], (uint32_t)(n / kTaRing) & 1u)) return ok = false;
+                    ++n;
+                    const int valid = it.n_keys - tile * kTaTile;
+                    if (value && it.fix_tail && valid < kTaTile) {
+                        for (int e = max(valid, 0) * 16 + lane; e < kTaTile * 16; e += 32)
+                            *reinterpret_cast<uint4 *>(sm.ring[slot] + ta_byte(e >> 4, e & 15)) = make_uint4(0, 0, 0, 0);
+                        proxy_fence();
+                        __syncwarp();
+                    }
+                }
+                if (value && !ta_wait_warp(sm, &sm.p_ready[s], c & 1)) return ok = false;
+                tc_fence_after();
+                if (lane == 0) {
+                    if (!value) {
+                        const uint64_t da = tc_desc_sw128(ta_addr(sm.q[it.shared ? s : 0]), 16, 1024), db = tc_desc_sw128(ta_addr(sm.ring[slot]), 16, 1024);
+#pragma unroll
+                        for (int x = 0; x < 8; ++x) {
+                            const uint64_t at = (uint64_t)(((x >> 2) * (kTaTileBytes / 2) + (x & 3) * 32) >> 4);
+                            tc_mma(sm.tmem + 128u * s, da + at, db + at, idesc_s, x > 0 ? 1u : 0u);
+                        }
+                        tc_commit(ta_addr(&sm.s_ready[s]));
+                    } else {
+                        const uint64_t db = tc_desc_sw128(ta_addr(sm.ring[slot]), kTaTileBytes / 2, 1024);
+#pragma unroll
+                        for (int x = 0; x < (kTwo ? 16 : 8); ++x)
+                            ta_mma_ts(sm.tmem + 256u + 128u * s, sm.tmem + 128u * s + 8u * x, db + (uint64_t)(((x & 7) * 2048) >> 4), idesc_o,
+                                      c > 0 || x > 0 ? 1u : 0u);
+                        if (c + 1 == it.count[s]) tc_commit(ta_addr(&sm.done[s]));
+                    }
+                    if (last) tc_commit(ta_addr(&sm.empty[slot]));
+                }
+                __syncwarp();
+                return true;
+            });
+        if (!ok) {                                         // products under way finish before their memory goes (a barrier nobody else waits for now)
+            if (lane == 0) {
+                tc_commit(ta_addr(&sm.q_ready));
+                for (int i = 0; i < 4096; ++i) __nanosleep(256);
+                if (sc.status != nullptr) atomicOr(sc.status, 4);
+            }
+            __syncwarp();
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (warp == 9) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(sm.tmem), "r"(512));
+}
+
+// O of the rows, out of tensor memory: put(column, 32 values times 1 / l (kNormal) or as they are, with m and l). Where the
+// streams are parts of the same rows stream 1's O goes through shared memory ([column][row], where the key and value tiles
+// were) and stream 0 puts both. All 256 softmax threads come here, whatever their waits said.
+template <bool kNormal, typename Put>
+__device__ __forceinline__ void ta_rows(TaSmem &sm, const TaItem &it, bool ok, int s, bool live, float m, float l, Put put)
+{
+    const int t = threadIdx.x & 127;
+    const uint32_t t_o = sm.tmem + ((uint32_t)((threadIdx.x >> 5) & 3) << 21) + 256u + 128u * s;
+    const bool warp_live = __any_sync(0xFFFFFFFFu, live);
+    float *other = reinterpret_cast<float *>(sm.ring[0]);
+    float2 *stat = reinterpret_cast<float2 *>(sm.q[1]);
+    float mine = 1.f, theirs = 0.f;
+    float o[32];
+    if (!it.shared) {
+        ta_named_barrier(1, 256);                          // both streams' products are over: the ring is free
+        if (s == 1) {
+            stat[t] = make_float2(m, l);
+            if (it.count[1] > 0 && warp_live)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    ta_ld32(t_o + 32 * q, o);
+                    ta_ld_wait();
+                    ta_tie(o);
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) other[(32 * q + i) * kTaTile + t] = o[i];
+                }
+        }
+        ta_named_barrier(1, 256);
+        if (s == 1) return;
+        const float2 b = stat[t];
+        const float top = fmaxf(m, b.x), ref = top == -CUDART_INF_F ? 0.f : top;
+        mine = ta_ex2(m - ref);
+        theirs = ta_ex2(b.x - ref);
+        l = l * mine + b.y * theirs;
+        m = top;
+        ok = ok && *reinterpret_cast<volatile int *>(&sm.failed) == 0;
+    }
+    if (!warp_live) return;
+    if (!ok) mine = CUDART_NAN_F, l = CUDART_NAN_F, m = 0.f;
+    if constexpr (kNormal) {
+        const float by = l == 0.f ? 0.f : 1.f / l;
+        mine *= by;
+        theirs *= by;
+    }
+    const bool both = !it.shared && it.count[1] > 0;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        ta_ld32(t_o + 32 * q, o);
+        ta_ld_wait();
+        ta_tie(o);
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+            o[i] *= mine;
+            if (both) o[i] = fmaf(theirs, other[(32 * q + i) * kTaTile + t], o[i]);
+        }
+        if (live) put(32 * q, o, m, l);
+    }
+}
+
+// Planes [n_planes][rows][128] of 16-bit values, plane_rows rows apart, as a tensor map with boxes of 64 values x 128 rows;
+// rows behind `rows` read as zeros. Returns false where the driver refuses.
+bool ta_tensor_map(CUtensorMap *map, const void *base, int64_t rows, int64_t plane_rows, int n_planes, bool half);
+int ta_score(const santapp_attn_opts *opts, TaScore *score);     // a santapp_status
+
+}  // namespace santapp

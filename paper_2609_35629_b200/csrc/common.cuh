@@ -218,6 +218,8 @@ inline cudaError_t launch_step(void (*kernel)(KArgs...), dim3 grid, dim3 block, 
 int note_cuda_failure(cudaError_t err, const char *where);     // records the text, returns SANTAPP_ERR_CUDA
 void note_launch_count(int n);
 int current_stage_mask();
+int check_geometry(const santapp_geom *g);                     // a santapp_status: what every call asks of its geometry
+void begin_call();                                             // no CUDA error, no launches yet
 
 // ---------------------------------------------------------------------------------------------
 // Host launchers (each returns the cudaError_t of its launches).

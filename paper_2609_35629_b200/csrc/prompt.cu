@@ -1,0 +1,170 @@
+// Attention of the prompts of a ragged batch (santapp_prompt_attn) on attn_tc.cuh.
+//
+// A block takes 256 query rows (a KV head's query heads of 256 / group tokens) of one sequence and every key tile that one of them sees:
+// 4 d operations per query head and visible pair, far more than the bytes, so tensor cores and exponentials bound
+// it. Blocks run from the longest sequence's last rows (which see most keys) down, so that the last ones are short.
+// The sequences' tables travel in the kernel's arguments, kPromptSeqs at a launch.
+#include <algorithm>
+#include <math.h>
+#include <string.h>
+#include <vector>
+
+#include "attn_tc.cuh"
+#include "santapp_serve.h"
+
+namespace santapp {
+
+namespace {
+
+constexpr int kPromptSeqs = 96;
+
+struct PromptSeq {
+    int key0, n_keys, token0, n_new, both, item0;
+};
+struct PromptParams {
+    const uint16_t *q;
+    uint16_t *out;
+    int n_q, n_kv, group, n_seqs;
+    TaScore score;
+    PromptSeq seq[kPromptSeqs];
+};
+
+template <bool kHalf, bool kCap, bool kBias>
+__global__ void __launch_bounds__(kTaThreads, 1)
+prompt_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map, const __grid_constant__ PromptParams p)
+{
+    step_wait();
+    extern __shared__ __align__(1024) unsigned char smem_prompt[];
+    TaSmem &sm = *reinterpret_cast<TaSmem *>(smem_prompt);
+    int lo = 0, hi = p.n_seqs - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) / 2;
+        if (p.seq[mid].item0 <= (int)blockIdx.x) lo = mid;
+        else hi = mid - 1;
+    }
+    const PromptSeq sq = p.seq[lo];
+    const int local = (int)blockIdx.x - sq.item0, n_rows = sq.n_new * p.group, j = local % p.n_kv;
+    TaItem it;
+    it.head0 = j * p.group;
+    it.group = p.group;
+    it.n_q = p.n_q;
+    it.q = p.q + (int64_t)sq.token0 * p.n_q * kHeadDim;
+    it.row0 = ((n_rows + 2 * kTaTile - 1) / (2 * kTaTile) - 1 - local / p.n_kv) * 2 * kTaTile;
+    it.n_rows = min(2 * kTaTile, n_rows - it.row0);
+    it.plane = j;
+    it.key0 = sq.key0;
+    it.n_keys = sq.n_keys;
+    it.tile0 = 0;
+    it.shared = it.n_rows > kTaTile;
+    it.fix_tail = true;
+    const auto seen = [&](int row) { return max(sq.n_keys - sq.n_new + row / p.group + 1, sq.both); };
+    const auto tiles = [&](int rows) { return (seen(it.row0 + rows - 1) + kTaTile - 1) / kTaTile; };
+    if (it.shared) {
+        it.count[0] = tiles(kTaTile);
+        it.count[1] = tiles(it.n_rows);
+    } else {
+        const int n = tiles(it.n_rows);
+        it.count[0] = (n + 1) / 2;
+        it.count[1] = n / 2;
+    }
+    ta_block<kHalf, false, kCap, kBias>(
+        sm, it, p.score, &k_map, &v_map, nullptr,
+        [&](int row, int &vis, int &q_pos) {
+            q_pos = sq.n_keys - sq.n_new + row / p.group;
+            vis = seen(row);
+        },
+        [&](bool ok, int s, int r, bool live, float m, float l) {
+            const int row = it.row0 + r;
+            uint16_t *dst = p.out + ((int64_t)(sq.token0 + row / p.group) * p.n_q + it.head0 + row % p.group) * kHeadDim;
+            ta_rows<true>(sm, it, ok, s, live, m, l, [&](int col, const float (&o)[32], float, float) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    reinterpret_cast<uint4 *>(dst + col)[i] =
+                        make_uint4(ta_pack<kHalf>(o[8 * i], o[8 * i + 1]), ta_pack<kHalf>(o[8 * i + 2], o[8 * i + 3]),
+                                   ta_pack<kHalf>(o[8 * i + 4], o[8 * i + 5]), ta_pack<kHalf>(o[8 * i + 6], o[8 * i + 7]));
+            });
+        });
+}
+
+bool misaligned(const void *p, size_t a) { return p != nullptr && (reinterpret_cast<uintptr_t>(p) % a) != 0; }
+
+using PromptKernel = void (*)(const CUtensorMap, const CUtensorMap, const PromptParams);
+template <bool kHalf>
+PromptKernel prompt_kernel_of(bool cap, bool bias)
+{
+    return cap ? (bias ? prompt_kernel<kHalf, true, true> : prompt_kernel<kHalf, true, false>)
+               : (bias ? prompt_kernel<kHalf, false, true> : prompt_kernel<kHalf, false, false>);
+}
+
+}  // namespace
+
+}  // namespace santapp
+
+using namespace santapp;
+
+extern "C" int santapp_prompt_attn(const santapp_geom *geom, const int32_t *prompt_len_host, const int32_t *new_len_host,
+                                   const int32_t *prefix_len_host, const void *q, const void *k_prompt, const void *v_prompt,
+                                   const santapp_attn_opts *opts, void *out, santapp_stream stream)
+{
+    int rc = check_geometry(geom);
+    if (rc != SANTAPP_OK) return rc;
+    TaScore score;
+    if ((rc = ta_score(opts, &score)) != SANTAPP_OK) return rc;
+    if (!prompt_len_host || !q || !k_prompt || !v_prompt || !out) return SANTAPP_ERR_INVALID_ARG;
+    if (misaligned(q, 16) || misaligned(k_prompt, 16) || misaligned(v_prompt, 16) || misaligned(out, 16)) return SANTAPP_ERR_INVALID_ARG;
+    const int B = geom->n_seqs, group = geom->n_q_heads / geom->n_kv_heads;
+    int64_t keys = 0, tokens = 0;
+    for (int b = 0; b < B; ++b) {
+        const int n = prompt_len_host[b], m = new_len_host ? new_len_host[b] : n, both = prefix_len_host ? prefix_len_host[b] : 0;
+        if (n < 1 || m < 0 || m > n || both < 0 || both > n) return SANTAPP_ERR_INVALID_ARG;
+        keys += n;
+        tokens += m;
+    }
+    if (keys >= (int64_t)1 << 30 || tokens * group >= (int64_t)1 << 30) return SANTAPP_ERR_UNSUPPORTED;
+    if ((tokens * group / (2 * kTaTile) + B) * geom->n_kv_heads >= (int64_t)1 << 31) return SANTAPP_ERR_UNSUPPORTED;
+    begin_call();
+    if (tokens == 0) return SANTAPP_OK;
+    CUtensorMap k_map, v_map;
+    if (!ta_tensor_map(&k_map, k_prompt, keys, keys, geom->n_kv_heads, geom->elem_type != 0)
+        || !ta_tensor_map(&v_map, v_prompt, keys, keys, geom->n_kv_heads, geom->elem_type != 0))
+        return note_cuda_failure(cudaErrorInvalidValue, "tensor maps");
+
+    PromptParams p;
+    memset(&p, 0, sizeof(p));
+    p.q = static_cast<const uint16_t *>(q);
+    p.out = static_cast<uint16_t *>(out);
+    p.n_q = geom->n_q_heads;
+    p.n_kv = geom->n_kv_heads;
+    p.group = group;
+    p.score = score;
+    const PromptKernel kernel = geom->elem_type ? prompt_kernel_of<true>(score.cap_log2 > 0.f, score.slopes != nullptr)
+                                                : prompt_kernel_of<false>(score.cap_log2 > 0.f, score.slopes != nullptr);
+    static std::atomic<unsigned long long> opted[8];
+    const int which = (geom->elem_type ? 4 : 0) + (score.cap_log2 > 0.f ? 2 : 0) + (score.slopes != nullptr ? 1 : 0);
+    cudaError_t err = ensure_dynamic_smem(reinterpret_cast<const void *>(kernel), kTaSmemBytes, opted[which]);
+    if (err != cudaSuccess) return note_cuda_failure(err, "prompt attention set-up");
+    int launches = 0, key0 = 0, token0 = 0;
+    for (int first = 0; first < B;) {
+        int n = 0, b = first;
+        for (; b < B && n < kPromptSeqs; ++b) {
+            const int m = new_len_host ? new_len_host[b] : prompt_len_host[b];
+            if (m > 0) p.seq[n++] = {key0, prompt_len_host[b], token0, m, prefix_len_host ? prefix_len_host[b] : 0, 0};
+            key0 += prompt_len_host[b];
+            token0 += m;
+        }
+        first = b;
+        if (n == 0) continue;
+        std::sort(p.seq, p.seq + n, [](const PromptSeq &x, const PromptSeq &y) { return x.n_keys != y.n_keys ? x.n_keys > y.n_keys : x.key0 < y.key0; });
+        int items = 0;
+        for (int i = 0; i < n; ++i) {
+            p.seq[i].item0 = items;
+            items += (p.seq[i].n_new * group + 2 * kTaTile - 1) / (2 * kTaTile) * geom->n_kv_heads;
+        }
+        p.n_seqs = n;
+        err = launch_step(kernel, dim3((unsigned)items), dim3(kTaThreads), kTaSmemBytes, static_cast<cudaStream_t>(stream), k_map, v_map, p);
+        if (err != cudaSuccess) return note_cuda_failure(err, "prompt attention launch");
+        ++launches;
+    }
+    note_launch_count(launches);
+    return SANTAPP_OK;
+}
