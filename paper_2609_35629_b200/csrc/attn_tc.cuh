@@ -30,17 +30,18 @@
 
 namespace santapp {
 
-constexpr int kTaThreads = 320;           // warps 0-3, 4-7: a row each of streams 0, 1; warp 8: copies; warp 9: products
+constexpr int kTaThreads = 384;           // warps 0-3, 4-7: a row per thread of streams 0, 1; warp 8: copies; warp 9: products
 constexpr int kTaTile = 128;              // query rows of a stream, keys of a tile
 constexpr int kTaTileBytes = kTaTile * kHeadDim * 2;
 constexpr int kTaRing = 5;                // tiles of keys or values under way
 constexpr float kTaSlack = 8.f;
+constexpr int kTaPolyEvery = 4;           // of so many pairs of exponentials one is computed by a polynomial
 
 struct TaSmem {
     alignas(1024) unsigned char q[2][kTaTileBytes];
     unsigned char ring[kTaRing][kTaTileBytes];
     uint64_t full[kTaRing], empty[kTaRing];   // a tile has landed; the products have left it
-    uint64_t q_ready, s_ready[2], p_ready[2], done[2];
+    uint64_t q_ready, s_ready[2], p_ready[2][2], done[2];      // p_ready: weights of keys 0-63, 64-127
     uint64_t pos_ready[2][2];
     alignas(16) float pos[2][2][kTaTile];                 // positions of the keys of a stream's tile, less n_keys; by tile parity
     uint32_t tmem;
@@ -60,7 +61,7 @@ struct TaItem {
     int key0;                 // plane row of key 0
     int n_keys;               // rows behind this belong to somebody else
     int tile0;                // first key tile
-    int count[2];             // key tiles of each stream
+    int count0, count1;       // key tiles of each stream
     bool shared;              // the streams are two row tiles over the same keys
     bool fix_tail;            // the planes hold rows behind n_keys: they are zeroed in V's last tile (0 times NaN is no 0)
 };
@@ -146,8 +147,14 @@ __device__ __forceinline__ void ta_named_barrier(int id, int threads) { asm vola
 // A wait returns false once any of the block's waits has run out.
 __device__ __forceinline__ bool ta_wait(TaSmem &sm, uint64_t *bar, uint32_t parity)
 {
-    if (*reinterpret_cast<volatile int *>(&sm.failed)) return false;
-    if (tc_wait(ta_addr(bar), parity)) return true;
+    const uint32_t b = ta_addr(bar);
+    for (int i = 0; i < (1 << 20); ++i) {
+        uint32_t over;
+        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.b32 %0, 1, 0, p;\n\t}\n"
+                     : "=r"(over) : "r"(b), "r"(parity) : "memory");
+        if (over) return true;
+        if (*reinterpret_cast<volatile int *>(&sm.failed)) return false;
+    }
     *reinterpret_cast<volatile int *>(&sm.failed) = 1;
     return false;
 }
@@ -156,23 +163,91 @@ __device__ __forceinline__ bool ta_wait_warp(TaSmem &sm, uint64_t *bar, uint32_t
 {
     return __all_sync(0xFFFFFFFFu, ta_wait(sm, bar, parity));
 }
+// One arrival for the warp, behind everything its lanes did.
+__device__ __forceinline__ void ta_arrive_warp(uint64_t *bar)
+{
+    __syncwarp();
+    if ((threadIdx.x & 31) == 0) mbar_arrive(ta_addr(bar));
+}
+__device__ __forceinline__ bool ta_elect()
+{
+    uint32_t p;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.b32 %0, 1, 0, p;\n\t}" : "=r"(p));
+    return p != 0;
+}
 
-// The order in which key and value tiles are first used, the same for the warp that copies and the one that issues products.
-// use(value?, tile, stream, c): stream's c-th tile as keys (false) or values (true).
+// ---- pairs of fp32 values in one instruction ----
+__device__ __forceinline__ uint64_t ta_two(float a, float b)
+{
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ void ta_split(uint64_t x, float &a, float &b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(x)); }
+__device__ __forceinline__ uint64_t ta_fma2(uint64_t a, uint64_t b, uint64_t c)
+{
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t ta_add2(uint64_t a, uint64_t b)
+{
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+// 2^x of a pair without the special-function unit: x = n + f, n whole, |f| <= 1/2; 2^f by the polynomial with the smallest largest relative
+// error (an exchange algorithm's: 2.7e-6 of degree 4, 2.3e-7 of degree 5, in fp32), n added to the exponent. x is at most
+// 127 and taken as -125 below that.
+template <int kDegree>
+__device__ __forceinline__ void ta_ex2_poly(uint64_t x, float &a, float &b)
+{
+    float x0, x1;
+    ta_split(x, x0, x1);
+    x = ta_two(fmaxf(x0, -125.f), fmaxf(x1, -125.f));
+    constexpr float kRound = 12582912.f;                    // 1.5 * 2^23: adding it leaves whole numbers
+    const uint64_t t = ta_add2(x, ta_two(kRound, kRound));
+    const uint64_t f = ta_add2(x, ta_fma2(t, ta_two(-1.f, -1.f), ta_two(kRound, kRound)));
+    const auto c = [](float v) { return ta_two(v, v); };
+    uint64_t r;
+    if constexpr (kDegree == 4) {
+        r = ta_fma2(c(0.009570101911165427f), f, c(0.055917860319388245f));
+        r = ta_fma2(r, f, c(0.2402474482786378f));
+        r = ta_fma2(r, f, c(0.6931218147366892f));
+        r = ta_fma2(r, f, c(0.9999992614457122f));
+    } else {
+        r = ta_fma2(c(0.0013276471992533984f), f, c(0.009675541334453752f));
+        r = ta_fma2(r, f, c(0.055507132734978495f));
+        r = ta_fma2(r, f, c(0.24022119723839974f));
+        r = ta_fma2(r, f, c(0.6931469670647609f));
+        r = ta_fma2(r, f, c(1.0000000716546849f));
+    }
+    float t0, t1, r0, r1;
+    ta_split(t, t0, t1);
+    ta_split(r, r0, r1);
+    a = __int_as_float(__float_as_int(r0) + (__float_as_int(t0) << 23));
+    b = __int_as_float(__float_as_int(r1) + (__float_as_int(t1) << 23));
+}
+
+// The order in which key and value tiles are first used, the same for the warp that copies and the one that issues products:
+// use(value?, stream, c) with stream's c-th tile as keys or values; the stream is a constant.
+template <int kStream> struct TaStream { static constexpr int value = kStream; };
 template <typename Use>
 __device__ __forceinline__ void ta_order(const TaItem &it, Use use)
 {
-    const int most = max(it.count[0], it.count[1]);
-    for (int s = 0; s < 2; ++s)
-        if (it.count[s] > 0)
-            if (!use(false, s, 0)) return;
-    for (int c = 0; c < most; ++c)
-        for (int s = 0; s < 2; ++s) {
-            if (c >= it.count[s]) continue;
-            if (!use(true, s, c)) return;
-            if (c + 1 < it.count[s])
-                if (!use(false, s, c + 1)) return;
+    if (it.count0 > 0 && !use(false, TaStream<0>{}, 0)) return;
+    if (it.count1 > 0 && !use(false, TaStream<1>{}, 0)) return;
+    const int most = max(it.count0, it.count1);
+    for (int c = 0; c < most; ++c) {
+        if (c < it.count0) {
+            if (!use(true, TaStream<0>{}, c)) return;
+            if (c + 1 < it.count0 && !use(false, TaStream<0>{}, c + 1)) return;
         }
+        if (c < it.count1) {
+            if (!use(true, TaStream<1>{}, c)) return;
+            if (c + 1 < it.count1 && !use(false, TaStream<1>{}, c + 1)) return;
+        }
+    }
 }
 
 // One stream's rows: thread t of 128 owns row t. `vis`: keys [0, vis) are seen by the row; q_pos its position; key_pos
@@ -188,7 +263,8 @@ __device__ __forceinline__ bool ta_softmax(TaSmem &sm, const TaItem &it, const T
     const bool warp_live = __any_sync(0xFFFFFFFFu, live);
     m = -CUDART_INF_F;
     l = 0.f;
-    for (int c = 0; c < it.count[s]; ++c) {
+    const int count = s ? it.count1 : it.count0;
+    for (int c = 0; c < count; ++c) {
         const int tile = it.tile0 + (it.shared ? c : 2 * c + s), kb = tile * kTaTile;
         if (kBias && key_pos != nullptr) {
             // (relative to n_keys, so that near keys of a very long prompt keep whole distances in fp32; who writes here has
@@ -240,9 +316,12 @@ __device__ __forceinline__ bool ta_softmax(TaSmem &sm, const TaItem &it, const T
 #pragma unroll
                 for (int i = 0; i < kTaTile; ++i) v[i] = i < seen ? v[i] : -CUDART_INF_F;
             }
-            float mx = v[0];
+            float top[4] = {v[0], v[1], v[2], v[3]};
 #pragma unroll
-            for (int i = 1; i < kTaTile; ++i) mx = fmaxf(mx, v[i]);
+            for (int i = 4; i < kTaTile; i += 8)
+#pragma unroll
+                for (int x = 0; x < 4; ++x) top[x] = i + 4 + x < kTaTile ? fmaxf(fmaxf(top[x], v[i + x]), v[i + 4 + x]) : fmaxf(top[x], v[i + x]);
+            float mx = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
             constexpr bool kRaw = !kCap && !kBias;          // v is in units of the product, not yet scaled
             if constexpr (kRaw) mx *= sc.scale_log2;
             const float m_new = fmaxf(m, mx);
@@ -264,29 +343,52 @@ __device__ __forceinline__ bool ta_softmax(TaSmem &sm, const TaItem &it, const T
                 m = m_new;
             }
             const float shift = kShift - (m == -CUDART_INF_F ? 0.f : m), mul = kRaw ? sc.scale_log2 : 1.f;
-            float sum[4] = {0.f, 0.f, 0.f, 0.f};
+            const uint64_t shift2 = ta_two(shift, shift), mul2 = ta_two(mul, mul);
+            uint64_t sum[2] = {0, 0};
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 uint32_t hi[16], lo[16];
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    const float p0 = ta_ex2(fmaf(v[32 * q + 2 * i], mul, shift)), p1 = ta_ex2(fmaf(v[32 * q + 2 * i + 1], mul, shift));
-                    sum[(2 * i) & 3] += p0;
-                    sum[(2 * i + 1) & 3] += p1;
+                    const uint64_t x = ta_fma2(ta_two(v[32 * q + 2 * i], v[32 * q + 2 * i + 1]), mul2, shift2);
+                    float p0, p1;
+                    if (i % kTaPolyEvery == kTaPolyEvery - 1) {
+                        ta_ex2_poly<kTwo ? 5 : 4>(x, p0, p1);
+                    } else {
+                        ta_split(x, p0, p1);
+                        p0 = ta_ex2(p0);
+                        p1 = ta_ex2(p1);
+                    }
+                    const uint64_t pp = ta_two(p0, p1);
+                    sum[i & 1] = ta_add2(sum[i & 1], pp);
                     hi[i] = ta_pack<kHalf>(p0, p1);
-                    if constexpr (kTwo) lo[i] = ta_pack<kHalf>(p0 - elem_lo<kHalf>(hi[i]), p1 - elem_hi<kHalf>(hi[i]));
+                    if constexpr (kTwo) {
+                        float d0, d1;
+                        ta_split(ta_fma2(ta_two(elem_lo<kHalf>(hi[i]), elem_hi<kHalf>(hi[i])), ta_two(-1.f, -1.f), pp), d0, d1);
+                        lo[i] = ta_pack<kHalf>(d0, d1);
+                    }
                 }
                 ta_st16(t_s + 16 * q, hi);
                 if constexpr (kTwo) ta_st16(t_s + 64 + 16 * q, lo);
+                if (q == 1) {
+                    ta_st_wait();
+                    tc_fence_before();
+                    ta_arrive_warp(&sm.p_ready[s][0]);
+                }
             }
-            l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+            float s0, s1;
+            ta_split(ta_add2(sum[0], sum[1]), s0, s1);
+            l += s0 + s1;
             ta_st_wait();
             tc_fence_before();
+            ta_arrive_warp(&sm.p_ready[s][1]);
+        } else {
+            ta_arrive_warp(&sm.p_ready[s][0]);
+            ta_arrive_warp(&sm.p_ready[s][1]);
         }
-        mbar_arrive(ta_addr(&sm.p_ready[s]));
     }
     m -= kShift;                                           // the factor of the weights is the sum's too
-    if (it.count[s] > 0) {
+    if (count > 0) {
         if (!ta_wait_warp(sm, &sm.done[s], 0)) return false;
         tc_fence_after();
     }
@@ -309,7 +411,7 @@ __device__ __forceinline__ void ta_block(TaSmem &sm, const TaItem &it, const TaS
         asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(ta_addr(&sm.q_ready)), "r"(256));
         for (int s = 0; s < 2; ++s) {
             asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(ta_addr(&sm.s_ready[s])), "r"(1));
-            asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(ta_addr(&sm.p_ready[s])), "r"(128));
+            for (int i = 0; i < 2; ++i) asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(ta_addr(&sm.p_ready[s][i])), "r"(4));
             asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(ta_addr(&sm.done[s])), "r"(1));
             for (int i = 0; i < 2; ++i) asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(ta_addr(&sm.pos_ready[s][i])), "r"(128));
         }
@@ -323,9 +425,12 @@ __device__ __forceinline__ void ta_block(TaSmem &sm, const TaItem &it, const TaS
     __syncthreads();
     tc_fence_after();
 
+    // registers: 168 a thread at launch; the softmax warps take what the other four leave (8 * 208 + 4 * 80 <= 12 * 168)
     if (warp < 8) {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
         // ---- the queries, then a row of scores per thread ----
         const int tiles = it.shared ? 2 : 1;
+#pragma unroll 4
         for (int e = tid; e < tiles * kTaTile * 16; e += 256) {
             const int r = e >> 4, ch = e & 15, row = it.row0 + r;
             uint4 x = make_uint4(0, 0, 0, 0);
@@ -343,80 +448,102 @@ __device__ __forceinline__ void ta_block(TaSmem &sm, const TaItem &it, const TaS
         if (kBias && live) slope = 1.4426950409f * sc.slopes[it.head0 + (it.row0 + r) % it.group];
         const bool ok = ta_softmax<kHalf, kTwo, kCap, kBias>(sm, it, sc, s, live, vis, q_pos, slope, key_pos, m, l);
         finish(ok, s, r, live, m, l);
-    } else if (warp == 8) {
-        // ---- copies: tiles in the order of their first use ----
-        if (lane == 0) {
-            int n = 0;                                     // tiles asked for
-            bool ok = true;
-            ta_order(it, [&](bool value, int s, int c) {
-                if (it.shared && s == 1 && c < it.count[0]) return true;       // stream 0 has asked for it
-                const int slot = n % kTaRing;
-                if (n >= kTaRing && !ta_wait(sm, &sm.empty[slot], (uint32_t)(n / kTaRing - 1) & 1u)) return ok = false;
-                const uint32_t bar = ta_addr(&sm.full[slot]), dst = ta_addr(sm.ring[slot]);
-                const int tile = it.tile0 + (it.shared ? c : 2 * c + s);
-                asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(kTaTileBytes) : "memory");
-                const CUtensorMap *map = value ? v_map : k_map;
-                ta_copy(dst, map, 0, it.key0 + tile * kTaTile, it.plane, bar);
-                ta_copy(dst + kTaTileBytes / 2, map, 64, it.key0 + tile * kTaTile, it.plane, bar);
-                ++n;
-                return true;
-            });
-            // nothing leaves while a copy is under way (in the normal course the products have waited for all of them)
-            for (int i = max(0, n - kTaRing); i < n; ++i) tc_wait(ta_addr(&sm.full[i % kTaRing]), (uint32_t)(i / kTaRing) & 1u);
-        }
     } else {
-        // ---- products ----
-        const uint32_t idesc_s = tc_idesc(kTaTile, kTaTile, 0, 0, kHalf), idesc_o = tc_idesc(kTaTile, kHeadDim, 0, 1, kHalf);
-        int n = 0, k_slot = 0, v_slot = 0;
-        bool ok = ta_wait_warp(sm, &sm.q_ready, 0);
-        if (ok)
-            ta_order(it, [&](bool value, int s, int c) {
-                int &slot = value ? v_slot : k_slot;
-                const int tile = it.tile0 + (it.shared ? c : 2 * c + s);
-                const bool first = !(it.shared && s == 1 && c < it.count[0]), last = !(it.shared && s == 0 && c < it.count[1]);
-                if (first) {
-                    slot = n % kTaRing;
-                    if (!ta_wait_warp(sm, &sm.full[slot], (uint32_t)(n / kTaRing) & 1u)) return ok = false;
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
+        if (warp == 8) {
+            // ---- copies: tiles in the order of their first use ----
+            if (ta_elect()) {
+                int n = 0, slot = 0;                       // tiles asked for; where the next goes
+                uint32_t phase = 0;
+                ta_order(it, [&](bool value, auto stream, int c) {
+                    constexpr int s = decltype(stream)::value;
+                    if (s == 1 && it.shared && c < it.count0) return true;       // stream 0 has asked for it
+                    if (n >= kTaRing && !ta_wait(sm, &sm.empty[slot], phase ^ 1u)) return false;
+                    const uint32_t bar = ta_addr(&sm.full[slot]), dst = ta_addr(sm.ring[slot]);
+                    const int y = it.key0 + (it.tile0 + (it.shared ? c : 2 * c + s)) * kTaTile;
+                    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(kTaTileBytes) : "memory");
+                    const CUtensorMap *map = value ? v_map : k_map;
+                    ta_copy(dst, map, 0, y, it.plane, bar);
+                    ta_copy(dst + kTaTileBytes / 2, map, 64, y, it.plane, bar);
                     ++n;
-                    const int valid = it.n_keys - tile * kTaTile;
-                    if (value && it.fix_tail && valid < kTaTile) {
-                        for (int e = max(valid, 0) * 16 + lane; e < kTaTile * 16; e += 32)
-                            *reinterpret_cast<uint4 *>(sm.ring[slot] + ta_byte(e >> 4, e & 15)) = make_uint4(0, 0, 0, 0);
-                        proxy_fence();
-                        __syncwarp();
-                    }
-                }
-                if (value && !ta_wait_warp(sm, &sm.p_ready[s], c & 1)) return ok = false;
-                tc_fence_after();
-                if (lane == 0) {
-                    if (!value) {
-                        const uint64_t da = tc_desc_sw128(ta_addr(sm.q[it.shared ? s : 0]), 16, 1024), db = tc_desc_sw128(ta_addr(sm.ring[slot]), 16, 1024);
-#pragma unroll
-                        for (int x = 0; x < 8; ++x) {
-                            const uint64_t at = (uint64_t)(((x >> 2) * (kTaTileBytes / 2) + (x & 3) * 32) >> 4);
-                            tc_mma(sm.tmem + 128u * s, da + at, db + at, idesc_s, x > 0 ? 1u : 0u);
-                        }
-                        tc_commit(ta_addr(&sm.s_ready[s]));
-                    } else {
-                        const uint64_t db = tc_desc_sw128(ta_addr(sm.ring[slot]), kTaTileBytes / 2, 1024);
-#pragma unroll
-                        for (int x = 0; x < (kTwo ? 16 : 8); ++x)
-                            ta_mma_ts(sm.tmem + 256u + 128u * s, sm.tmem + 128u * s + 8u * x, db + (uint64_t)(((x & 7) * 2048) >> 4), idesc_o,
-                                      c > 0 || x > 0 ? 1u : 0u);
-                        if (c + 1 == it.count[s]) tc_commit(ta_addr(&sm.done[s]));
-                    }
-                    if (last) tc_commit(ta_addr(&sm.empty[slot]));
-                }
-                __syncwarp();
-                return true;
-            });
-        if (!ok) {                                         // products under way finish before their memory goes (a barrier nobody else waits for now)
-            if (lane == 0) {
-                tc_commit(ta_addr(&sm.q_ready));
-                for (int i = 0; i < 4096; ++i) __nanosleep(256);
-                if (sc.status != nullptr) atomicOr(sc.status, 4);
+                    if (++slot == kTaRing) slot = 0, phase ^= 1u;
+                    return true;
+                });
+                // nothing leaves while a copy is under way (in the normal course the products have waited for all of them)
+                for (int i = max(0, n - kTaRing); i < n; ++i) tc_wait(ta_addr(&sm.full[i % kTaRing]), (uint32_t)(i / kTaRing) & 1u);
             }
             __syncwarp();
+        } else if (warp == 9) {
+            // ---- products ----
+            const uint32_t tmem = __shfl_sync(0xFFFFFFFFu, sm.tmem, 0);
+            const uint32_t idesc_s = tc_idesc(kTaTile, kTaTile, 0, 0, kHalf), idesc_o = tc_idesc(kTaTile, kHeadDim, 0, 1, kHalf);
+            const uint64_t q_desc = tc_desc_sw128(ta_addr(sm.q[0]), 16, 1024), k_desc = tc_desc_sw128(ta_addr(sm.ring[0]), 16, 1024);
+            const uint64_t v_desc = tc_desc_sw128(ta_addr(sm.ring[0]), kTaTileBytes / 2, 1024);
+            int next = 0, k_slot = 0, v_slot = 0;
+            uint32_t phase = 0;
+            bool ok = ta_wait_warp(sm, &sm.q_ready, 0);
+            if (ok)
+                ta_order(it, [&](bool value, auto stream, int c) {
+                    constexpr int s = decltype(stream)::value;
+                    const bool first = !(s == 1 && it.shared && c < it.count0), last = !(s == 0 && it.shared && c < it.count1);
+                    if (first) {
+                        if (!ta_wait_warp(sm, &sm.full[next], phase)) return ok = false;
+                        if (value) v_slot = next;
+                        else k_slot = next;
+                        if (++next == kTaRing) next = 0, phase ^= 1u;
+                    }
+                    if (!value) {
+                        tc_fence_after();
+                        if (ta_elect()) {
+                            const uint64_t da = q_desc + (uint64_t)((s == 1 && it.shared ? kTaTileBytes : 0) >> 4), db = k_desc + (uint64_t)((k_slot * kTaTileBytes) >> 4);
+#pragma unroll
+                            for (int x = 0; x < 8; ++x) {
+                                const uint64_t at = (uint64_t)(((x >> 2) * (kTaTileBytes / 2) + (x & 3) * 32) >> 4);
+                                tc_mma(tmem + 128u * s, da + at, db + at, idesc_s, x > 0 ? 1u : 0u);
+                            }
+                            tc_commit(ta_addr(&sm.s_ready[s]));
+                            if (last) tc_commit(ta_addr(&sm.empty[k_slot]));
+                        }
+                        __syncwarp();
+                        return true;
+                    }
+                    if (first && it.fix_tail) {
+                        const int valid = it.n_keys - (it.tile0 + (it.shared ? c : 2 * c + s)) * kTaTile;
+                        if (valid < kTaTile) {
+                            for (int e = max(valid, 0) * 16 + lane; e < kTaTile * 16; e += 32)
+                                *reinterpret_cast<uint4 *>(sm.ring[v_slot] + ta_byte(e >> 4, e & 15)) = make_uint4(0, 0, 0, 0);
+                            proxy_fence();
+                            __syncwarp();
+                        }
+                    }
+                    const uint64_t db = v_desc + (uint64_t)((v_slot * kTaTileBytes) >> 4);
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) {
+                        if (!ta_wait_warp(sm, &sm.p_ready[s][half], c & 1)) return ok = false;
+                        tc_fence_after();
+                        if (ta_elect()) {
+#pragma unroll
+                            for (int x = 4 * half; x < 4 * half + 4; ++x)
+#pragma unroll
+                                for (int term = 0; term < (kTwo ? 2 : 1); ++term)
+                                    ta_mma_ts(tmem + 256u + 128u * s, tmem + 128u * s + 64u * term + 8u * x, db + (uint64_t)((x * 2048) >> 4), idesc_o,
+                                              c > 0 || x > 0 || term > 0 ? 1u : 0u);
+                            if (half == 1) {
+                                if (c + 1 == (s ? it.count1 : it.count0)) tc_commit(ta_addr(&sm.done[s]));
+                                if (last) tc_commit(ta_addr(&sm.empty[v_slot]));
+                            }
+                        }
+                        __syncwarp();
+                    }
+                    return true;
+                });
+            if (!ok) {                                     // products under way finish before their memory goes
+                if (lane == 0) {
+                    for (int i = 0; i < 4096; ++i) __nanosleep(256);
+                    if (sc.status != nullptr) atomicOr(sc.status, 4);
+                }
+                __syncwarp();
+            }
         }
     }
     tc_fence_before();
@@ -442,7 +569,7 @@ __device__ __forceinline__ void ta_rows(TaSmem &sm, const TaItem &it, bool ok, i
         ta_named_barrier(1, 256);                          // both streams' products are over: the ring is free
         if (s == 1) {
             stat[t] = make_float2(m, l);
-            if (it.count[1] > 0 && warp_live)
+            if (it.count1 > 0 && warp_live)
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
                     ta_ld32(t_o + 32 * q, o);
@@ -469,7 +596,7 @@ __device__ __forceinline__ void ta_rows(TaSmem &sm, const TaItem &it, bool ok, i
         mine *= by;
         theirs *= by;
     }
-    const bool both = !it.shared && it.count[1] > 0;
+    const bool both = !it.shared && it.count1 > 0;
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
         ta_ld32(t_o + 32 * q, o);

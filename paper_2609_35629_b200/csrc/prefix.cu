@@ -69,8 +69,8 @@ prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__
     it.tile0 = t0;
     it.shared = it.n_rows > kTaTile;
     it.fix_tail = false;                                    // (the tensor map ends at the last row)
-    it.count[0] = it.shared ? t1 - t0 : (t1 - t0 + 1) / 2;
-    it.count[1] = it.shared ? t1 - t0 : (t1 - t0) / 2;
+    it.count0 = it.shared ? t1 - t0 : (t1 - t0 + 1) / 2;
+    it.count1 = it.shared ? t1 - t0 : (t1 - t0) / 2;
     const int32_t *key_pos = kBias && p.key_pos != nullptr ? p.key_pos + (int64_t)j * p.plane_rows : nullptr;
     ta_block<kHalf, true, kCap, kBias>(
         sm, it, p.score, &k_map, &v_map, key_pos,

@@ -60,12 +60,12 @@ prompt_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__
     const auto seen = [&](int row) { return max(sq.n_keys - sq.n_new + row / p.group + 1, sq.both); };
     const auto tiles = [&](int rows) { return (seen(it.row0 + rows - 1) + kTaTile - 1) / kTaTile; };
     if (it.shared) {
-        it.count[0] = tiles(kTaTile);
-        it.count[1] = tiles(it.n_rows);
+        it.count0 = tiles(kTaTile);
+        it.count1 = tiles(it.n_rows);
     } else {
         const int n = tiles(it.n_rows);
-        it.count[0] = (n + 1) / 2;
-        it.count[1] = n / 2;
+        it.count0 = (n + 1) / 2;
+        it.count1 = n / 2;
     }
     ta_block<kHalf, false, kCap, kBias>(
         sm, it, p.score, &k_map, &v_map, nullptr,
