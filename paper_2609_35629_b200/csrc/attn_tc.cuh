@@ -30,8 +30,8 @@
 
 namespace santapp {
 
-constexpr int kTaThreads = 384;           // warps 0-3, 4-7: a row per thread of streams 0, 1; warp 8: copies; warp 9: products;
-                                          // warp 10: the last tile's rows that are somebody else's
+constexpr int kTaThreads = 384;           // warps 0-3, 4-7: a row per thread of streams 0, 1; warp 8: copies; warp 9: products; warp 10: the
+                                          // last tile's rows that are somebody else's
 constexpr int kTaTile = 128;              // query rows of a stream, keys of a tile
 constexpr int kTaTileBytes = kTaTile * kHeadDim * 2;
 constexpr int kTaRing = 5;                // tiles of keys or values under way
@@ -92,11 +92,19 @@ __device__ __forceinline__ uint32_t ta_pack(float lo, float hi)
     else                 asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
     return r;
 }
-// A operand in tensor memory
-__device__ __forceinline__ void ta_mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate)
+// Products whose descriptors differ in their lower words alone (addresses): between two of them the issuing lane has two additions to
+// make. (With 64-bit descriptors and a predicate computed for each, 16 of them took 90 to 99 cycles each beside nothing, 64 this way.)
+__device__ __forceinline__ void ta_mma_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t upper, uint32_t idesc, uint32_t accumulate)
 {
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-                 "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}\n" ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate)
+    asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\tsetp.ne.b32 p, %5, 0;\n\tmov.b64 a, {%1, %3};\n\tmov.b64 b, {%2, %3};\n\t"
+                 "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %4, p;\n\t}\n" ::"r"(d), "r"(a), "r"(b), "r"(upper), "r"(idesc), "r"(accumulate)
+                 : "memory");
+}
+// A in tensor memory
+__device__ __forceinline__ void ta_mma_ts(uint32_t d, uint32_t a, uint32_t b, uint32_t upper, uint32_t idesc, uint32_t accumulate)
+{
+    asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 b;\n\tsetp.ne.b32 p, %5, 0;\n\tmov.b64 b, {%2, %3};\n\t"
+                 "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %4, p;\n\t}\n" ::"r"(d), "r"(a), "r"(b), "r"(upper), "r"(idesc), "r"(accumulate)
                  : "memory");
 }
 // 32 columns, on their way until ta_ld_wait
@@ -245,26 +253,16 @@ __device__ __forceinline__ void ta_ex2_poly(uint64_t x, float &a, float &b)
     b = __int_as_float(__float_as_int(r1) + (__float_as_int(t1) << 23));
 }
 
-// The order in which key and value tiles are first used, the same for the warp that copies and the one that issues products:
-// use(value?, stream, c) with stream's c-th tile as keys or values; the stream is a constant.
 template <int kStream> struct TaStream { static constexpr int value = kStream; };
-template <typename Use>
-__device__ __forceinline__ void ta_order(const TaItem &it, Use use)
+// Place of a tile in the order in which the ring is filled, which is that of first use: K_0 V_0 K_1 V_1 ... where both streams use
+// a tile, K_0 K_1 V_0 K_2 V_1 K_3 ... where they take tiles in turn. Slot: place % kTaRing.
+__device__ __forceinline__ int ta_tiles(const TaItem &it) { return it.shared ? it.count1 : it.count0 + it.count1; }
+__device__ __forceinline__ int ta_key_place(const TaItem &it, int tile) { return it.shared ? 2 * tile : max(2 * tile - 1, 0); }
+__device__ __forceinline__ int ta_value_place(const TaItem &it, int tile)
 {
-    if (it.count0 > 0 && !use(false, TaStream<0>{}, 0)) return;
-    if (it.count1 > 0 && !use(false, TaStream<1>{}, 0)) return;
-    const int most = max(it.count0, it.count1);
-    for (int c = 0; c < most; ++c) {
-        if (c < it.count0) {
-            if (!use(true, TaStream<0>{}, c)) return;
-            if (c + 1 < it.count0 && !use(false, TaStream<0>{}, c + 1)) return;
-        }
-        if (c < it.count1) {
-            if (!use(true, TaStream<1>{}, c)) return;
-            if (c + 1 < it.count1 && !use(false, TaStream<1>{}, c + 1)) return;
-        }
-    }
+    return it.shared ? 2 * tile + 1 : min(2 * tile + 2, 2 * ta_tiles(it) - 1);
 }
+__device__ __forceinline__ bool ta_cut(const TaItem &it) { return it.fix_tail && it.n_keys < (it.tile0 + ta_tiles(it)) * kTaTile; }
 
 // cap * tanh(x cap_in) * log2 e of a thread's 128 products. |x cap_in| <= 1 throughout the warp, the usual case: tanh(y) = y P(y^2), P with the
 // smallest largest relative error (degree 5 in y^2: 6e-7; 6: 5e-8), cap * log2 e folded into its coefficients. Otherwise from e = exp(-2 |y|):
@@ -493,11 +491,12 @@ __device__ __forceinline__ void ta_block(TaSmem &sm, const TaItem &it, const TaS
         const int tiles = it.shared ? 2 : 1;
 #pragma unroll 4
         for (int e = tid; e < tiles * kTaTile * 16; e += 256) {
-            const int r = e >> 4, ch = e & 15, row = it.row0 + r;
-            uint4 x = make_uint4(0, 0, 0, 0);
-            if (r < it.n_rows) x = reinterpret_cast<const uint4 *>(it.q + ((int64_t)(row / it.group) * it.n_q + it.head0 + row % it.group) * kHeadDim)[ch];
-            *reinterpret_cast<uint4 *>(sm.q[r >> 7] + ta_byte(r & 127, ch)) = x;
+            const int r = e >> 4, ch = e & 15, row = it.row0 + min(r, it.n_rows - 1);
+            const uint16_t *src = it.q + ((int64_t)(row / it.group) * it.n_q + it.head0 + row % it.group) * kHeadDim + 8 * ch;
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(ta_addr(sm.q[r >> 7] + ta_byte(r & 127, ch))), "l"(src),
+                         "r"(r < it.n_rows ? 16 : 0) : "memory");
         }
+        asm volatile("cp.async.wait_all;" ::: "memory");
         proxy_fence();
         mbar_arrive(ta_addr(&sm.q_ready));
         const int s = warp >> 2, r = (tid & 127) + (it.shared ? kTaTile * s : 0);
@@ -512,109 +511,114 @@ __device__ __forceinline__ void ta_block(TaSmem &sm, const TaItem &it, const TaS
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
         if (warp == 8) {
-            // ---- copies: tiles in the order of their first use ----
+            // ---- copies ----
             if (ta_elect()) {
-                int n = 0, slot = 0;                       // tiles asked for; where the next goes
-                uint32_t phase = 0;
-                ta_order(it, [&](bool value, auto stream, int c) {
-                    constexpr int s = decltype(stream)::value;
-                    if (s == 1 && it.shared && c < it.count0) return true;       // stream 0 has asked for it
-                    if (n >= kTaRing && !ta_wait(sm, &sm.empty[slot], phase ^ 1u)) return false;
-                    const int first_key = (it.tile0 + (it.shared ? c : 2 * c + s)) * kTaTile, y = it.key0 + first_key;
+                int n = 0;                                 // tiles asked for
+                const int n_tiles = ta_tiles(it);
+                const bool cut = ta_cut(it);
+                const auto ask = [&](bool value, int tile) {
+                    const int slot = n % kTaRing;
+                    if (n >= kTaRing && !ta_wait(sm, &sm.empty[slot], (uint32_t)(n / kTaRing - 1) & 1u)) return false;
                     // (warp 10 hands on a tile of values that ends in somebody else's rows)
-                    const uint32_t bar = ta_addr(value && it.fix_tail && first_key + kTaTile > it.n_keys ? &sm.tail : &sm.full[slot]), dst = ta_addr(sm.ring[slot]);
+                    const uint32_t bar = ta_addr(value && cut && tile == n_tiles - 1 ? &sm.tail : &sm.full[slot]), dst = ta_addr(sm.ring[slot]);
+                    const int y = it.key0 + (it.tile0 + tile) * kTaTile;
                     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(kTaTileBytes) : "memory");
                     const CUtensorMap *map = value ? v_map : k_map;
                     ta_copy(dst, map, 0, y, it.plane, bar);
                     ta_copy(dst + kTaTileBytes / 2, map, 64, y, it.plane, bar);
                     ++n;
-                    if (++slot == kTaRing) slot = 0, phase ^= 1u;
                     return true;
-                });
+                };
+                bool ok = true;
+                if (!it.shared) ok = ask(false, 0);
+                for (int i = 0; ok && i < n_tiles; ++i) {
+                    const int keys = it.shared ? i : i + 1;
+                    if (keys < n_tiles) ok = ask(false, keys);
+                    ok = ok && ask(true, i);
+                }
                 // nothing leaves while a copy is under way (in the normal course the products have waited for all of them)
                 for (int i = max(0, n - kTaRing); i < n; ++i) tc_wait(ta_addr(&sm.full[i % kTaRing]), (uint32_t)(i / kTaRing) & 1u);
             }
             __syncwarp();
         } else if (warp == 9) {
-            // ---- products: one lane, so that a wait costs no votes (the tensor core's queue holds about four instructions, 256
-            // cycles: what lies between two groups has to be shorter) ----
+            // ---- products: one lane. Strictly in turn, stream 0's weights with its values and its next scores, then stream 1's: when both
+            // streams' weights are there at once, one still gets its scores a thousand cycles before the other, and its exponentials
+            // are taken while the other's products run (a warp per stream left both waiting for one another's halves: 515 us for 481) ----
             const uint32_t tmem = __shfl_sync(0xFFFFFFFFu, sm.tmem, 0);
             if (ta_elect()) {
                 const uint32_t idesc_s = tc_idesc(kTaTile, kTaTile, 0, 0, kHalf), idesc_o = tc_idesc(kTaTile, kHeadDim, 0, 1, kHalf);
-                const uint64_t q_desc = tc_desc_sw128(ta_addr(sm.q[0]), 16, 1024), k_desc = tc_desc_sw128(ta_addr(sm.ring[0]), 16, 1024);
-                const uint64_t v_desc = tc_desc_sw128(ta_addr(sm.ring[0]), kTaTileBytes / 2, 1024);
-                int next = 0, k_slot = 0, v_slot = 0;
-                uint32_t phase = 0;
-                bool ahead = false;                        // the next tile has been waited for
+                // (lower words: address / 16, leading offset)
+                const uint32_t q_low = (uint32_t)tc_desc_sw128(ta_addr(sm.q[0]), 16, 1024), k_low = (uint32_t)tc_desc_sw128(ta_addr(sm.ring[0]), 16, 1024);
+                const uint32_t v_low = (uint32_t)tc_desc_sw128(ta_addr(sm.ring[0]), kTaTileBytes / 2, 1024), upper = (uint32_t)(tc_desc_sw128(0, 16, 1024) >> 32);
+                const uint32_t q1_low = q_low + (it.shared ? kTaTileBytes >> 4 : 0);
+                const auto landed = [&](int place) { return ta_wait(sm, &sm.full[place % kTaRing], (uint32_t)(place / kTaRing) & 1u); };
+                // a tile's last use of the two: what was issued so far over, its slot is free
+                const auto leave = [&](int s, int c, int place) {
+                    if (s == 1 || !it.shared || c >= it.count1) tc_commit(ta_addr(&sm.empty[place % kTaRing]));
+                };
+                const auto scores = [&](auto stream, int c) {
+                    constexpr int s = decltype(stream)::value;
+                    const int place = ta_key_place(it, it.shared ? c : 2 * c + s);
+                    const uint32_t a = s ? q1_low : q_low, b = k_low + (uint32_t)(place % kTaRing * (kTaTileBytes >> 4));
+#pragma unroll
+                    for (int x = 0; x < 8; ++x) {
+                        const uint32_t at = ((x >> 2) * (kTaTileBytes / 2) + (x & 3) * 32) >> 4;
+                        ta_mma_ss(tmem + 128u * s, a + at, b + at, upper, idesc_s, x > 0 ? 1u : 0u);
+                    }
+                    tc_commit(ta_addr(&sm.s_ready[s]));
+                    leave(s, c, place);
+                };
+                const auto values = [&](auto stream, int c) {
+                    constexpr int s = decltype(stream)::value;
+                    const int count = s ? it.count1 : it.count0, tile = it.shared ? c : 2 * c + s, place = ta_value_place(it, tile);
+                    const uint32_t b = v_low + (uint32_t)(place % kTaRing * (kTaTileBytes >> 4));
+                    if (!landed(place)) return false;
+#pragma unroll
+                    for (int part = 0; part < 2; ++part) {                  // keys 0 .. 95, 96 .. 127
+                        if (!ta_wait(sm, &sm.p_ready[s][part], c & 1)) return false;
+                        tc_fence_after();
+#pragma unroll
+                        for (int x = 6 * part; x < (part ? 8 : 6); ++x)
+#pragma unroll
+                            for (int term = 0; term < (kTwo ? 2 : 1); ++term)
+                                ta_mma_ts(tmem + 256u + 128u * s, tmem + 128u * s + 64u * term + 8u * x, b + ((x * 2048) >> 4), upper, idesc_o,
+                                          x > 0 || term > 0 ? 1u : (c > 0 ? 1u : 0u));
+                        // (the keys of the product behind this one)
+                        if (part == 0 && c + 1 < count && !landed(ta_key_place(it, it.shared ? c + 1 : 2 * c + 2 + s))) return false;
+                    }
+                    if (c + 1 == count) tc_commit(ta_addr(&sm.done[s]));
+                    leave(s, c, place);
+                    if (c + 1 < count) scores(stream, c + 1);
+                    return true;
+                };
                 bool ok = ta_wait(sm, &sm.q_ready, 0);
-                if (ok)
-                    ta_order(it, [&](bool value, auto stream, int c) {
-                        constexpr int s = decltype(stream)::value;
-                        const bool first = !(s == 1 && it.shared && c < it.count0), last = !(s == 0 && it.shared && c < it.count1);
-                        if (first) {
-                            if (!ahead && !ta_wait(sm, &sm.full[next], phase)) return ok = false;
-                            ahead = false;
-                            if (value) v_slot = next;
-                            else k_slot = next;
-                            if (++next == kTaRing) next = 0, phase ^= 1u;
-                        }
-                        if (!value) {
-                            tc_fence_after();
-                            const uint64_t da = q_desc + (uint64_t)((s == 1 && it.shared ? kTaTileBytes : 0) >> 4), db = k_desc + (uint64_t)((k_slot * kTaTileBytes) >> 4);
-#pragma unroll
-                            for (int x = 0; x < 8; ++x) {
-                                const uint64_t at = (uint64_t)(((x >> 2) * (kTaTileBytes / 2) + (x & 3) * 32) >> 4);
-                                tc_mma(tmem + 128u * s, da + at, db + at, idesc_s, x > 0 ? 1u : 0u);
-                            }
-                            tc_commit(ta_addr(&sm.s_ready[s]));
-                            if (last) tc_commit(ta_addr(&sm.empty[k_slot]));
-                            return true;
-                        }
-                        const uint64_t db = v_desc + (uint64_t)((v_slot * kTaTileBytes) >> 4);
-#pragma unroll
-                        for (int half = 0; half < 2; ++half) {        // keys 0 .. 95, 96 .. 127
-                            if (half == 1 && c + 1 < (s ? it.count1 : it.count0) && !(s == 1 && it.shared && c + 1 < it.count0)) {
-                                if (!ta_wait(sm, &sm.full[next], phase)) return ok = false;      // the keys of the product behind this one
-                                ahead = true;
-                            }
-                            if (!ta_wait(sm, &sm.p_ready[s][half], c & 1)) return ok = false;
-                            tc_fence_after();
-#pragma unroll
-                            for (int x = 6 * half; x < (half ? 8 : 6); ++x)
-#pragma unroll
-                                for (int term = 0; term < (kTwo ? 2 : 1); ++term)
-                                    ta_mma_ts(tmem + 256u + 128u * s, tmem + 128u * s + 64u * term + 8u * x, db + (uint64_t)((x * 2048) >> 4), idesc_o,
-                                              c > 0 || x > 0 || term > 0 ? 1u : 0u);
-                        }
-                        if (c + 1 == (s ? it.count1 : it.count0)) tc_commit(ta_addr(&sm.done[s]));
-                        if (last) tc_commit(ta_addr(&sm.empty[v_slot]));
-                        return true;
-                    });
+                if (ok && it.count0 > 0 && (ok = landed(0))) {
+                    tc_fence_after();
+                    scores(TaStream<0>{}, 0);
+                }
+                if (ok && it.count1 > 0 && (ok = landed(ta_key_place(it, it.shared ? 0 : 1)))) {
+                    tc_fence_after();
+                    scores(TaStream<1>{}, 0);
+                }
+                for (int c = 0; ok && c < max(it.count0, it.count1); ++c) {
+                    if (c < it.count0) ok = values(TaStream<0>{}, c);
+                    if (ok && c < it.count1) ok = values(TaStream<1>{}, c);
+                }
                 if (!ok) {                                 // products under way finish before their memory goes
                     for (int i = 0; i < 4096; ++i) __nanosleep(256);
                     if (sc.status != nullptr) atomicOr(sc.status, 4);
                 }
             }
             __syncwarp();
-        } else if (warp == 10 && it.fix_tail) {
+        } else if (warp == 10 && ta_cut(it)) {
             // ---- the rows behind the last one, in the last tile of values ----
-            int slot = 0;
-            ta_order(it, [&](bool value, auto stream, int c) {
-                constexpr int s = decltype(stream)::value;
-                if (s == 1 && it.shared && c < it.count0) return true;
-                const int valid = it.n_keys - (it.tile0 + (it.shared ? c : 2 * c + s)) * kTaTile;
-                if (value && valid < kTaTile) {
-                    if (ta_wait_warp(sm, &sm.tail, 0)) {
-                        for (int e = max(valid, 0) * 16 + lane; e < kTaTile * 16; e += 32)
-                            *reinterpret_cast<uint4 *>(sm.ring[slot] + ta_byte(e >> 4, e & 15)) = make_uint4(0, 0, 0, 0);
-                        proxy_fence();
-                        ta_arrive_warp(&sm.full[slot]);
-                    }
-                    return false;
-                }
-                if (++slot == kTaRing) slot = 0;
-                return true;
-            });
+            const int place = 2 * ta_tiles(it) - 1, valid = it.n_keys - (it.tile0 + ta_tiles(it) - 1) * kTaTile;
+            if (ta_wait_warp(sm, &sm.tail, 0)) {
+                for (int e = max(valid, 0) * 16 + lane; e < kTaTile * 16; e += 32)
+                    *reinterpret_cast<uint4 *>(sm.ring[place % kTaRing] + ta_byte(e >> 4, e & 15)) = make_uint4(0, 0, 0, 0);
+                proxy_fence();
+                ta_arrive_warp(&sm.full[place % kTaRing]);
+            }
         }
     }
     tc_fence_before();
