@@ -10,7 +10,9 @@
 //   O += P V         P from tensor memory, V as it lies in memory (N-major)
 // While the tensor core does stream 0's O += P V and its next S, the other stream's warps take their exponentials.
 // With more than 128 query rows the streams are two row tiles over the same keys (a tile of keys is fetched
-// once for both); with fewer they take the key tiles of the same rows in turn and are joined at the end.
+// once for both); with fewer they take the key tiles of the same rows in turn and are joined at the end. Rows that fill
+// half or a quarter of a tile are in it two or four times (fold), each time with weights for one half or quarter of the keys and
+// zeros for the others: a thread has 64 or 32 exponentials to take where the tensor core has idle rows anyway.
 //
 // Weights: kTwo splits a weight into two 16-bit terms, p = hi + lo (off by at most 2^-16 of it, bf16), two products with V:
 // outputs good to fp32. Without, a weight is rounded once (2^-8, bf16), for outputs that are 16 bits wide anyway.
@@ -64,6 +66,7 @@ struct TaItem {
     int tile0;                // first key tile
     int count0, count1;       // key tiles of each stream
     bool shared;              // the streams are two row tiles over the same keys
+    int fold;                 // not shared: the 128 lanes hold the rows 1, 2 or 4 times, each time for another part of a tile's keys
     bool fix_tail;            // the planes hold rows behind n_keys: they are zeroed in V's last tile (0 times NaN is no 0)
 };
 struct TaScore {
@@ -264,11 +267,11 @@ __device__ __forceinline__ int ta_value_place(const TaItem &it, int tile)
 }
 __device__ __forceinline__ bool ta_cut(const TaItem &it) { return it.fix_tail && it.n_keys < (it.tile0 + ta_tiles(it)) * kTaTile; }
 
-// cap * tanh(x cap_in) * log2 e of a thread's 128 products. |x cap_in| <= 1 throughout the warp, the usual case: tanh(y) = y P(y^2), P with the
+// cap * tanh(x cap_in) * log2 e of a thread's products. |x cap_in| <= 1 throughout the warp, the usual case: tanh(y) = y P(y^2), P with the
 // smallest largest relative error (degree 5 in y^2: 6e-7; 6: 5e-8), cap * log2 e folded into its coefficients. Otherwise from e = exp(-2 |y|):
 // (1 - e) / (1 + e) with y's sign, two uses of the special-function unit.
-template <bool kTwo>
-__device__ __forceinline__ void ta_cap(const TaScore &sc, float (&v)[kTaTile])
+template <bool kTwo, int kCols>
+__device__ __forceinline__ void ta_cap(const TaScore &sc, float (&v)[kCols])
 {
     constexpr int kN = kTwo ? 7 : 6;
     constexpr float kP[2][7] = {{0.9999994135992578f, -0.3332904237853047f, 0.13281433880736535f, -0.05160567400212715f, 0.016743115063748693f, -0.0030670603265534825f, 0.f},
@@ -276,14 +279,14 @@ __device__ __forceinline__ void ta_cap(const TaScore &sc, float (&v)[kTaTile])
                                  -0.006203379104680566f, 0.0010410226337084262f}};
     float far = 0.f;
 #pragma unroll
-    for (int i = 0; i < kTaTile; i += 2) far = fmaxf(fmaxf(far, fabsf(v[i])), fabsf(v[i + 1]));
+    for (int i = 0; i < kCols; i += 2) far = fmaxf(fmaxf(far, fabsf(v[i])), fabsf(v[i + 1]));
     if (__all_sync(0xFFFFFFFFu, far * sc.cap_in <= 1.f)) {
         uint64_t c[kN];
 #pragma unroll
         for (int k = 0; k < kN; ++k) c[k] = ta_two(kP[kTwo][k] * sc.cap_log2, kP[kTwo][k] * sc.cap_log2);
         const uint64_t in = ta_two(sc.cap_in, sc.cap_in);
 #pragma unroll
-        for (int i = 0; i < kTaTile; i += 2) {
+        for (int i = 0; i < kCols; i += 2) {
             const uint64_t y = ta_mul2(ta_two(v[i], v[i + 1]), in), u = ta_mul2(y, y);
             uint64_t r = c[kN - 1];
 #pragma unroll
@@ -292,7 +295,7 @@ __device__ __forceinline__ void ta_cap(const TaScore &sc, float (&v)[kTaTile])
         }
     } else {
 #pragma unroll
-        for (int i = 0; i < kTaTile; ++i) {
+        for (int i = 0; i < kCols; ++i) {
             const float y = v[i] * sc.cap_in, e = ta_ex2(-2.885390082f * fabsf(y));
             v[i] = copysignf(__fdividef(1.f - e, 1.f + e), y) * sc.cap_log2;
         }
@@ -306,7 +309,7 @@ __device__ __forceinline__ void ta_cap(const TaScore &sc, float (&v)[kTaTile])
 // exponentials is taken against the maximum of the tiles before, beside the search for this tile's; where a score passes it by
 // more than 2^kTaSlack, and in the first tile, that quarter is taken again. The last quarter of the weights is handed over on its own: only
 // its product remains to be done when the last weight is there.
-template <bool kHalf, bool kTwo, bool kCap, bool kBias>
+template <bool kHalf, bool kTwo, bool kCap, bool kBias, int kCols>
 __device__ __forceinline__ bool ta_softmax(TaSmem &sm, const TaItem &it, const TaScore &sc, int s, bool live, int vis, int q_pos,
                                            float slope_log2, const int32_t *key_pos, float &m, float &l)
 {
@@ -315,6 +318,7 @@ __device__ __forceinline__ bool ta_softmax(TaSmem &sm, const TaItem &it, const T
     const int t = threadIdx.x & 127;
     const uint32_t lanes = (uint32_t)((threadIdx.x >> 5) & 3) << 21;
     const uint32_t t_s = sm.tmem + lanes + 128u * s, t_o = sm.tmem + lanes + 256u + 128u * s;
+    const int col0 = t / kCols * kCols;      // first of the keys of a tile that this thread weighs
     const bool warp_live = __any_sync(0xFFFFFFFFu, live);
     m = -CUDART_INF_F;
     l = 0.f;
@@ -324,47 +328,47 @@ __device__ __forceinline__ bool ta_softmax(TaSmem &sm, const TaItem &it, const T
         ta_named_barrier(2 + s, 128);
     }
     for (int c = 0; c < count; ++c) {
-        const int kb = (it.tile0 + (it.shared ? c : 2 * c + s)) * kTaTile;
+        const int tile = (it.tile0 + (it.shared ? c : 2 * c + s)) * kTaTile, kb = tile + col0;
         if (kBias && key_pos != nullptr) {
             // (relative to n_keys, so that near keys of a very long prompt keep whole distances in fp32; who writes here has
             // seen all 128 threads at the tile before this one, that is behind the reading of the tile before that)
-            sm.pos[s][c & 1][t] = kb + t < it.n_keys ? (float)(key_pos[kb + t] - it.n_keys) : 0.f;
+            sm.pos[s][c & 1][t] = tile + t < it.n_keys ? (float)(key_pos[tile + t] - it.n_keys) : 0.f;
             mbar_arrive(ta_addr(&sm.pos_ready[s][c & 1]));
             if (!ta_wait_warp(sm, &sm.pos_ready[s][c & 1], (uint32_t)(c >> 1) & 1u)) return false;
         }
         if (!ta_wait_warp(sm, &sm.s_ready[s], c & 1)) return false;
         if (warp_live) {
             tc_fence_after();
-            float v[kTaTile];
+            float v[kCols];
 #pragma unroll
-            for (int q = 0; q < 4; ++q) ta_ld32(t_s + 32 * q, v + 32 * q);
+            for (int q = 0; q < kCols / 32; ++q) ta_ld32(t_s + col0 + 32 * q, v + 32 * q);
             ta_ld_wait();
 #pragma unroll
-            for (int q = 0; q < 4; ++q) ta_tie(v + 32 * q);
+            for (int q = 0; q < kCols / 32; ++q) ta_tie(v + 32 * q);
             if constexpr (kCap) ta_cap<kTwo>(sc, v);
             if constexpr (kBias) {
                 // linear in the key's position as long as no key is behind the query
                 const bool table = key_pos != nullptr;
-                const float *pos = sm.pos[s][table ? c & 1 : 0];
+                const float *pos = sm.pos[s][table ? c & 1 : 0] + (table ? col0 : 0);
                 const uint64_t slope2 = ta_two(slope_log2, slope_log2), mul2 = kCap ? ta_two(1.f, 1.f) : ta_two(sc.scale_log2, sc.scale_log2);
                 const float d = (float)(table ? q_pos - it.n_keys : q_pos - kb);
-                if (table || !__any_sync(0xFFFFFFFFu, live && min(vis, kb + kTaTile) - 1 > q_pos)) {
+                if (table || !__any_sync(0xFFFFFFFFu, live && min(vis, kb + kCols) - 1 > q_pos)) {
                     const uint64_t base = ta_two(-slope_log2 * d, -slope_log2 * d);
 #pragma unroll
-                    for (int i = 0; i < kTaTile; i += 4) {
+                    for (int i = 0; i < kCols; i += 4) {
                         const ulonglong2 p = *reinterpret_cast<const ulonglong2 *>(pos + i);
                         ta_split(ta_fma2(slope2, p.x, ta_fma2(ta_two(v[i], v[i + 1]), mul2, base)), v[i], v[i + 1]);
                         ta_split(ta_fma2(slope2, p.y, ta_fma2(ta_two(v[i + 2], v[i + 3]), mul2, base)), v[i + 2], v[i + 3]);
                     }
                 } else {
 #pragma unroll
-                    for (int i = 0; i < kTaTile; ++i) v[i] = fmaf(-slope_log2, fabsf(d - (float)i), kCap ? v[i] : v[i] * sc.scale_log2);
+                    for (int i = 0; i < kCols; ++i) v[i] = fmaf(-slope_log2, fabsf(d - (float)i), kCap ? v[i] : v[i] * sc.scale_log2);
                 }
             }
             const int seen = vis - kb;
-            if (__any_sync(0xFFFFFFFFu, seen < kTaTile)) {
+            if (__any_sync(0xFFFFFFFFu, seen < kCols)) {
 #pragma unroll
-                for (int i = 0; i < kTaTile; ++i) v[i] = i < seen ? v[i] : -CUDART_INF_F;
+                for (int i = 0; i < kCols; ++i) v[i] = i < seen ? v[i] : -CUDART_INF_F;
             }
             const float mul = kRaw ? sc.scale_log2 : 1.f;
             const uint64_t mul2 = ta_two(mul, mul);
@@ -393,17 +397,17 @@ __device__ __forceinline__ bool ta_softmax(TaSmem &sm, const TaItem &it, const T
                 }
             };
             const auto store = [&](int q) {
-                ta_st16(t_s + 16 * q, hi);
-                if constexpr (kTwo) ta_st16(t_s + 64 + 16 * q, lo);
+                ta_st16(t_s + col0 / 2 + 16 * q, hi);
+                if constexpr (kTwo) ta_st16(t_s + 64 + col0 / 2 + 16 * q, lo);
             };
             float shift = kShift - (m == -CUDART_INF_F ? 0.f : m);
             sum[0] = sum[1] = 0;
             weights(0, ta_two(shift, shift));
             float top[4] = {v[0], v[1], v[2], v[3]};
 #pragma unroll
-            for (int i = 4; i < kTaTile; i += 8)
+            for (int i = 4; i < kCols; i += 8)
 #pragma unroll
-                for (int x = 0; x < 4; ++x) top[x] = i + 4 + x < kTaTile ? fmaxf(fmaxf(top[x], v[i + x]), v[i + 4 + x]) : fmaxf(top[x], v[i + x]);
+                for (int x = 0; x < 4; ++x) top[x] = i + 4 + x < kCols ? fmaxf(fmaxf(top[x], v[i + x]), v[i + 4 + x]) : fmaxf(top[x], v[i + x]);
             const float m_new = fmaxf(m, mul * fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])));
             if (__any_sync(0xFFFFFFFFu, m_new > m + (c == 0 ? 0.f : kTaSlack))) {
                 if (c > 0) {
@@ -425,20 +429,37 @@ __device__ __forceinline__ bool ta_softmax(TaSmem &sm, const TaItem &it, const T
             }
             const uint64_t shift2 = ta_two(shift, shift);
             store(0);
-            weights(1, shift2);
-            store(1);
-            weights(2, shift2);
-            store(2);
-            ta_st_wait();
-            tc_fence_before();
-            ta_arrive_warp(&sm.p_ready[s][0]);
-            weights(3, shift2);
-            store(3);
+            if constexpr (kCols == kTaTile) {
+                weights(1, shift2);
+                store(1);
+                weights(2, shift2);
+                store(2);
+                ta_st_wait();
+                tc_fence_before();
+                ta_arrive_warp(&sm.p_ready[s][0]);
+                weights(3, shift2);
+                store(3);
+            } else {
+                if constexpr (kCols == 64) {
+                    weights(1, shift2);
+                    store(1);
+                }
+                // nothing for the keys that other lanes of this row weigh
+#pragma unroll
+                for (int i = 0; i < 16; ++i) hi[i] = 0u;
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    if (32 * q < col0 || 32 * q >= col0 + kCols) {
+                        ta_st16(t_s + 16 * q, hi);
+                        if constexpr (kTwo) ta_st16(t_s + 64 + 16 * q, hi);
+                    }
+            }
             float s0, s1;
             ta_split(ta_add2(sum[0], sum[1]), s0, s1);
             l += s0 + s1;
             ta_st_wait();
             tc_fence_before();
+            if constexpr (kCols != kTaTile) ta_arrive_warp(&sm.p_ready[s][0]);
             ta_arrive_warp(&sm.p_ready[s][1]);
         } else {
             ta_arrive_warp(&sm.p_ready[s][0]);
@@ -453,9 +474,9 @@ __device__ __forceinline__ bool ta_softmax(TaSmem &sm, const TaItem &it, const T
     return true;
 }
 
-// The block: set-up, copies, products. `rows(row, vis, q_pos)` tells how many keys a row sees and its position; `finish(ok, s, r, live, m, l)`
-// gets the statistics of stream s's row r of the item and takes O out of tensor memory (ta_rows).
-template <bool kHalf, bool kTwo, bool kCap, bool kBias, typename Rows, typename Finish>
+// The block: set-up, copies, products. `rows(row, vis, q_pos)` tells how many keys a row sees and its position; `finish(ok, s, live, m, l)`
+// gets the statistics of the thread's row and takes O out of tensor memory (ta_rows). kCols: keys of a tile that a thread weighs, 128 / fold.
+template <bool kHalf, bool kTwo, bool kCap, bool kBias, int kCols, typename Rows, typename Finish>
 __device__ __forceinline__ void ta_block(TaSmem &sm, const TaItem &it, const TaScore &sc, const CUtensorMap *k_map, const CUtensorMap *v_map,
                                          const int32_t *key_pos, Rows rows, Finish finish)
 {
@@ -491,23 +512,23 @@ __device__ __forceinline__ void ta_block(TaSmem &sm, const TaItem &it, const TaS
         const int tiles = it.shared ? 2 : 1;
 #pragma unroll 4
         for (int e = tid; e < tiles * kTaTile * 16; e += 256) {
-            const int r = e >> 4, ch = e & 15, row = it.row0 + min(r, it.n_rows - 1);
+            const int r = e >> 4, ch = e & 15, lr = it.shared ? r : r % (kTaTile / it.fold), row = it.row0 + min(lr, it.n_rows - 1);
             const uint16_t *src = it.q + ((int64_t)(row / it.group) * it.n_q + it.head0 + row % it.group) * kHeadDim + 8 * ch;
             asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(ta_addr(sm.q[r >> 7] + ta_byte(r & 127, ch))), "l"(src),
-                         "r"(r < it.n_rows ? 16 : 0) : "memory");
+                         "r"(lr < it.n_rows ? 16 : 0) : "memory");
         }
         asm volatile("cp.async.wait_all;" ::: "memory");
         proxy_fence();
         mbar_arrive(ta_addr(&sm.q_ready));
-        const int s = warp >> 2, r = (tid & 127) + (it.shared ? kTaTile * s : 0);
+        const int s = warp >> 2, r = it.shared ? (tid & 127) + kTaTile * s : (tid & 127) % (kTaTile / it.fold);
         bool live = r < it.n_rows;
         int vis = it.n_keys;
         int q_pos = 0;
         float slope = 0.f, m, l;
         if (live) rows(it.row0 + r, vis, q_pos);
         if (kBias && live) slope = 1.4426950409f * sc.slopes[it.head0 + (it.row0 + r) % it.group];
-        const bool ok = ta_softmax<kHalf, kTwo, kCap, kBias>(sm, it, sc, s, live, vis, q_pos, slope, key_pos, m, l);
-        finish(ok, s, r, live, m, l);
+        const bool ok = ta_softmax<kHalf, kTwo, kCap, kBias, kCols>(sm, it, sc, s, live, vis, q_pos, slope, key_pos, m, l);
+        finish(ok, s, live, m, l);
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
         if (warp == 8) {
@@ -627,62 +648,77 @@ __device__ __forceinline__ void ta_block(TaSmem &sm, const TaItem &it, const TaS
     if (warp == 9) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(sm.tmem), "r"(512));
 }
 
-// O of the rows, out of tensor memory: put(column, 32 values times 1 / l (kNormal) or as they are, with m and l). Where the
-// streams are parts of the same rows stream 1's O goes through shared memory ([column][row], where the key and value tiles
-// were) and stream 0 puts both. All 256 softmax threads come here, whatever their waits said.
+// O of the rows, out of tensor memory: put(row of the item, lane, its four values of the row, m, l), a row per warp at a time, O times 1 / l
+// (kNormal) or as it is. Parts of one row (the two streams where they take tiles in turn, and its copies in the tile) are joined here. Through
+// shared memory, where the queries and the key and value tiles were, so that a row leaves as one piece of memory. All 256 softmax
+// threads come here, whatever their waits said.
+constexpr int kTaPitch = kHeadDim + 4;
+static_assert(2 * kTaTile * kTaPitch * 4 <= kTaRing * kTaTileBytes, "O of both streams fits the ring");
 template <bool kNormal, typename Put>
 __device__ __forceinline__ void ta_rows(TaSmem &sm, const TaItem &it, bool ok, int s, bool live, float m, float l, Put put)
 {
-    const int t = threadIdx.x & 127;
-    const uint32_t t_o = sm.tmem + ((uint32_t)((threadIdx.x >> 5) & 3) << 21) + 256u + 128u * s;
-    const bool warp_live = __any_sync(0xFFFFFFFFu, live);
-    float *other = reinterpret_cast<float *>(sm.ring[0]);
-    float2 *stat = reinterpret_cast<float2 *>(sm.q[1]);
-    float mine = 1.f, theirs = 0.f;
-    float o[32];
-    if (!it.shared) {
-        ta_named_barrier(1, 256);                          // both streams' products are over: the ring is free
-        if (s == 1) {
-            stat[t] = make_float2(m, l);
-            if (it.count1 > 0 && warp_live)
+    const int t = threadIdx.x & 127, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    float *rows = reinterpret_cast<float *>(sm.ring[0]);
+    float2 *stat = reinterpret_cast<float2 *>(sm.q[0]);
+    ta_named_barrier(1, 256);                              // both streams' products are over
+    {
+        const uint32_t t_o = sm.tmem + ((uint32_t)(warp & 3) << 21) + 256u + 128u * s;
+        float *dst = rows + (kTaTile * s + t) * kTaPitch;
+        if ((s ? it.count1 : it.count0) > 0 && __any_sync(0xFFFFFFFFu, live)) {
+            float o[32];
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    ta_ld32(t_o + 32 * q, o);
-                    ta_ld_wait();
-                    ta_tie(o);
+            for (int q = 0; q < 4; ++q) {
+                ta_ld32(t_o + 32 * q, o);
+                ta_ld_wait();
+                ta_tie(o);
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) other[(32 * q + i) * kTaTile + t] = o[i];
-                }
+                for (int i = 0; i < 32; i += 4) *reinterpret_cast<float4 *>(dst + 32 * q + i) = make_float4(o[i], o[i + 1], o[i + 2], o[i + 3]);
+            }
         }
-        ta_named_barrier(1, 256);
-        if (s == 1) return;
-        const float2 b = stat[t];
-        const float top = fmaxf(m, b.x), ref = top == -CUDART_INF_F ? 0.f : top;
-        mine = ta_ex2(m - ref);
-        theirs = ta_ex2(b.x - ref);
-        l = l * mine + b.y * theirs;
-        m = top;
-        ok = ok && *reinterpret_cast<volatile int *>(&sm.failed) == 0;
+        stat[kTaTile * s + t] = ok ? make_float2(m, l) : make_float2(0.f, CUDART_NAN_F);
     }
-    if (!warp_live) return;
-    if (!ok) mine = CUDART_NAN_F, l = CUDART_NAN_F, m = 0.f;
-    if constexpr (kNormal) {
-        const float by = l == 0.f ? 0.f : 1.f / l;
-        mine *= by;
-        theirs *= by;
-    }
-    const bool both = !it.shared && it.count1 > 0;
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-        ta_ld32(t_o + 32 * q, o);
-        ta_ld_wait();
-        ta_tie(o);
-#pragma unroll
-        for (int i = 0; i < 32; ++i) {
-            o[i] *= mine;
-            if (both) o[i] = fmaf(theirs, other[(32 * q + i) * kTaTile + t], o[i]);
+    ta_named_barrier(1, 256);
+    const auto leave = [&](int r, float4 x, float top, float sum) {
+        if constexpr (kNormal) {
+            const float by = sum == 0.f ? 0.f : __fdividef(1.f, sum);
+            x.x *= by;
+            x.y *= by;
+            x.z *= by;
+            x.w *= by;
         }
-        if (live) put(32 * q, o, m, l);
+        put(r, lane, x, top, sum);
+    };
+    if (it.shared) {
+#pragma unroll 4
+        for (int i = 0; i < kTaTile / 4; ++i) {
+            const int r = 8 * i + warp;
+            if (r >= it.n_rows) continue;
+            const float2 st = stat[r];
+            leave(r, st.y != st.y ? make_float4(st.y, st.y, st.y, st.y) : reinterpret_cast<const float4 *>(rows + r * kTaPitch)[lane], st.x, st.y);
+        }
+        return;
+    }
+    const int copy = kTaTile / it.fold;
+#pragma unroll 2
+    for (int i = 0; i < kTaTile / 8; ++i) {
+        const int r = 8 * i + warp;
+        if (r >= it.n_rows) continue;
+        float top = -CUDART_INF_F, sum = 0.f;
+        for (int e = r; e < 2 * kTaTile; e += copy) top = fmaxf(top, stat[e].x);
+        const float ref = top == -CUDART_INF_F ? 0.f : top;
+        float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int e = r; e < 2 * kTaTile; e += copy) {
+            const float2 st = stat[e];
+            if (st.y == 0.f) continue;                     // (no key seen; where a stream has no tile, nothing was written)
+            const float w = st.y != st.y ? st.y : ta_ex2(st.x - ref);
+            const float4 y = reinterpret_cast<const float4 *>(rows + e * kTaPitch)[lane];
+            sum = fmaf(w, st.y, sum);
+            x.x = fmaf(w, y.x, x.x);
+            x.y = fmaf(w, y.y, x.y);
+            x.z = fmaf(w, y.z, x.z);
+            x.w = fmaf(w, y.w, x.w);
+        }
+        leave(r, x, top, sum);
     }
 }
 

@@ -47,11 +47,13 @@ __device__ __forceinline__ int suffix_rows(const PrefixParams &p, int b)
     return p.suffix_len != nullptr ? min(max(p.suffix_len[b], 0), p.suffix_cap) : 0;
 }
 
-template <bool kHalf, bool kCap, bool kBias>
+template <bool kHalf, bool kCap, bool kBias, int kFold>
 __global__ void __launch_bounds__(kTaThreads, 1)
 prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map, const __grid_constant__ PrefixParams p)
 {
     step_wait();
+    // (finish_kernel's blocks may come as this one's leave: they begin with the suffixes, which nothing here writes)
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     extern __shared__ __align__(1024) unsigned char smem_prefix[];
     TaSmem &sm = *reinterpret_cast<TaSmem *>(smem_prefix);
     const int part = blockIdx.x, j = blockIdx.y % p.n_kv, pair = blockIdx.y / p.n_kv;
@@ -67,23 +69,22 @@ prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__
     it.key0 = 0;
     it.n_keys = p.n_keys;
     it.tile0 = t0;
-    it.shared = it.n_rows > kTaTile;
+    it.shared = kFold == 1 && it.n_rows > kTaTile;
+    it.fold = kFold;
     it.fix_tail = false;                                    // (the tensor map ends at the last row)
     it.count0 = it.shared ? t1 - t0 : (t1 - t0 + 1) / 2;
     it.count1 = it.shared ? t1 - t0 : (t1 - t0) / 2;
     const int32_t *key_pos = kBias && p.key_pos != nullptr ? p.key_pos + (int64_t)j * p.plane_rows : nullptr;
-    ta_block<kHalf, true, kCap, kBias>(
+    ta_block<kHalf, true, kCap, kBias, kTaTile / kFold>(
         sm, it, p.score, &k_map, &v_map, key_pos,
         [&](int row, int &, int &q_pos) {
             if (kBias) q_pos = p.n_keys + suffix_rows(p, row / p.group) - 1;
         },
-        [&](bool ok, int s, int r, bool live, float m, float l) {
-            const int64_t slot = ((int64_t)j * p.parts + part) * p.rows + it.row0 + r;
-            ta_rows<false>(sm, it, ok, s, live, m, l, [&](int col, const float (&o)[32], float top, float sum) {
-                float4 *dst = reinterpret_cast<float4 *>(p.part_o + slot * kHeadDim + col);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) dst[i] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
-                if (col == 0) p.part_ml[slot] = make_float2(top, sum);
+        [&](bool ok, int s, bool live, float m, float l) {
+            ta_rows<false>(sm, it, ok, s, live, m, l, [&](int r, int lane, const float4 &o, float top, float sum) {
+                const int64_t slot = ((int64_t)j * p.parts + part) * p.rows + it.row0 + r;
+                reinterpret_cast<float4 *>(p.part_o + slot * kHeadDim)[lane] = o;
+                if (lane == 0) p.part_ml[slot] = make_float2(top, sum);
             });
         });
 }
@@ -149,7 +150,9 @@ template <bool kHalf, bool kCap, bool kBias>
 __global__ void __launch_bounds__(kFinishThreads)
 finish_kernel(const __grid_constant__ PrefixParams p)
 {
-    step_wait();
+    // The prefix kernel asks for this one once it has begun itself, behind everything before it on the stream: what it does not write is
+    // there. Without a prefix kernel this is the call's first.
+    if (p.parts == 0) step_wait();
     extern __shared__ __align__(1024) unsigned char smem_finish[];
     FinishSmem &sm = *reinterpret_cast<FinishSmem *>(smem_finish);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -263,36 +266,45 @@ finish_kernel(const __grid_constant__ PrefixParams p)
         if ((lane & 3) == 0) *reinterpret_cast<float2 *>(e + kHeadDim) = make_float2(m == -CUDART_INF_F ? m : m - kShift, l);
     }
 
-    // ---- partials share, share + shares, ... of the pair's rows ----
+    // ---- partials share, share + shares, ... of the pair's rows, the next one's on its way ----
+    if (p.parts > 0) step_wait();
     {
         const int64_t first = (int64_t)j * p.parts * p.rows + (int64_t)b * G;
         float top[kMaxGroup], sum[kMaxGroup];
-        float4 acc[kMaxGroup];
+        float4 acc[kMaxGroup], x[kMaxGroup];
+        float2 ml = make_float2(-CUDART_INF_F, 0.f);
+        const auto fetch_part = [&](int i) {
+            if (i >= p.parts) return;
+            const int64_t slot = first + (int64_t)i * p.rows;
+            ml = p.part_ml[slot + min(lane, G - 1)];
+#pragma unroll
+            for (int h = 0; h < kMaxGroup; ++h)
+                if (h < G) x[h] = reinterpret_cast<const float4 *>(p.part_o + (slot + h) * kHeadDim)[lane];
+        };
 #pragma unroll
         for (int h = 0; h < kMaxGroup; ++h) {
             top[h] = -CUDART_INF_F;
             sum[h] = 0.f;
-            acc[h] = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (h < G) {
-                for (int i = share + lane * shares; i < p.parts; i += 32 * shares) top[h] = fmaxf(top[h], p.part_ml[first + (int64_t)i * p.rows + h].x);
-#pragma unroll
-                for (int d = 16; d > 0; d >>= 1) top[h] = fmaxf(top[h], __shfl_xor_sync(0xFFFFFFFFu, top[h], d));
-            }
+            acc[h] = x[h] = make_float4(0.f, 0.f, 0.f, 0.f);
         }
+        fetch_part(share);
         for (int i = share; i < p.parts; i += shares) {
-            const int64_t slot = first + (int64_t)i * p.rows;
+            const float2 ml_now = ml;
+            float4 now[kMaxGroup];
+#pragma unroll
+            for (int h = 0; h < kMaxGroup; ++h) now[h] = x[h];
+            fetch_part(i + shares);
 #pragma unroll
             for (int h = 0; h < kMaxGroup; ++h) {
-                if (h >= G) continue;
-                const float2 ml = p.part_ml[slot + h];
-                const float4 x = reinterpret_cast<const float4 *>(p.part_o + (slot + h) * kHeadDim)[lane];
-                if (ml.x == -CUDART_INF_F) continue;
-                const float w = ta_ex2(ml.x - top[h]);
-                sum[h] = fmaf(w, ml.y, sum[h]);
-                acc[h].x = fmaf(w, x.x, acc[h].x);
-                acc[h].y = fmaf(w, x.y, acc[h].y);
-                acc[h].z = fmaf(w, x.z, acc[h].z);
-                acc[h].w = fmaf(w, x.w, acc[h].w);
+                const float mm = __shfl_sync(0xFFFFFFFFu, ml_now.x, h), ll = __shfl_sync(0xFFFFFFFFu, ml_now.y, h);
+                if (h >= G || mm == -CUDART_INF_F) continue;
+                const float t = fmaxf(top[h], mm), a = ta_ex2(top[h] - t), w = ta_ex2(mm - t);
+                top[h] = t;
+                sum[h] = fmaf(w, ll, sum[h] * a);
+                acc[h].x = fmaf(w, now[h].x, acc[h].x * a);
+                acc[h].y = fmaf(w, now[h].y, acc[h].y * a);
+                acc[h].z = fmaf(w, now[h].z, acc[h].z * a);
+                acc[h].w = fmaf(w, now[h].w, acc[h].w * a);
             }
         }
 #pragma unroll
@@ -397,13 +409,19 @@ int check_prefix(const santapp_geom *geom, int64_t n_keys, int suffix_cap)
 
 using PrefixKernel = void (*)(const CUtensorMap, const CUtensorMap, const PrefixParams);
 using FinishKernel = void (*)(const PrefixParams);
-template <bool kHalf>
-void prefix_kernels_of(bool cap, bool bias, PrefixKernel *a, FinishKernel *b)
+template <bool kHalf, bool kCap, bool kBias>
+void kernels_of(int fold, PrefixKernel *a, FinishKernel *b)
 {
-    *a = cap ? (bias ? prefix_kernel<kHalf, true, true> : prefix_kernel<kHalf, true, false>)
-             : (bias ? prefix_kernel<kHalf, false, true> : prefix_kernel<kHalf, false, false>);
-    *b = cap ? (bias ? finish_kernel<kHalf, true, true> : finish_kernel<kHalf, true, false>)
-             : (bias ? finish_kernel<kHalf, false, true> : finish_kernel<kHalf, false, false>);
+    *a = fold == 4 ? prefix_kernel<kHalf, kCap, kBias, 4> : (fold == 2 ? prefix_kernel<kHalf, kCap, kBias, 2> : prefix_kernel<kHalf, kCap, kBias, 1>);
+    *b = finish_kernel<kHalf, kCap, kBias>;
+}
+template <bool kHalf>
+void kernels_of(bool cap, bool bias, int fold, PrefixKernel *a, FinishKernel *b)
+{
+    if (cap && bias) kernels_of<kHalf, true, true>(fold, a, b);
+    else if (cap)    kernels_of<kHalf, true, false>(fold, a, b);
+    else if (bias)   kernels_of<kHalf, false, true>(fold, a, b);
+    else             kernels_of<kHalf, false, false>(fold, a, b);
 }
 
 }  // namespace
@@ -501,12 +519,13 @@ int santapp_prefix_decode_attn(const santapp_geom *geom, const void *k_prefix, c
     const bool cap = p.score.cap_log2 > 0.f, bias = p.score.slopes != nullptr, half = geom->elem_type != 0;
     PrefixKernel prefix;
     FinishKernel finish;
-    if (half) prefix_kernels_of<true>(cap, bias, &prefix, &finish);
-    else      prefix_kernels_of<false>(cap, bias, &prefix, &finish);
-    static std::atomic<unsigned long long> opted[2][8];
+    const int fold = p.rows <= kTaTile / 4 ? 4 : (p.rows <= kTaTile / 2 ? 2 : 1);
+    if (half) kernels_of<true>(cap, bias, fold, &prefix, &finish);
+    else      kernels_of<false>(cap, bias, fold, &prefix, &finish);
+    static std::atomic<unsigned long long> opted[4][8];
     const int which = (half ? 4 : 0) + (cap ? 2 : 0) + (bias ? 1 : 0);
-    cudaError_t err = ensure_dynamic_smem(reinterpret_cast<const void *>(prefix), kTaSmemBytes, opted[0][which]);
-    if (err == cudaSuccess) err = ensure_dynamic_smem(reinterpret_cast<const void *>(finish), (int)sizeof(FinishSmem), opted[1][which]);
+    cudaError_t err = ensure_dynamic_smem(reinterpret_cast<const void *>(prefix), kTaSmemBytes, opted[fold == 4 ? 2 : fold - 1][which]);
+    if (err == cudaSuccess) err = ensure_dynamic_smem(reinterpret_cast<const void *>(finish), (int)sizeof(FinishSmem), opted[3][which]);
     if (err != cudaSuccess) return note_cuda_failure(err, "prefix attention set-up");
     int launches = 0;
     if (L.parts > 0) {

@@ -56,6 +56,7 @@ prompt_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__
     it.n_keys = sq.n_keys;
     it.tile0 = 0;
     it.shared = it.n_rows > kTaTile;
+    it.fold = 1;
     it.fix_tail = true;
     const auto seen = [&](int row) { return max(sq.n_keys - sq.n_new + row / p.group + 1, sq.both); };
     const auto tiles = [&](int rows) { return (seen(it.row0 + rows - 1) + kTaTile - 1) / kTaTile; };
@@ -67,21 +68,17 @@ prompt_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__
         it.count0 = (n + 1) / 2;
         it.count1 = n / 2;
     }
-    ta_block<kHalf, false, kCap, kBias>(
+    ta_block<kHalf, false, kCap, kBias, kTaTile>(
         sm, it, p.score, &k_map, &v_map, nullptr,
         [&](int row, int &vis, int &q_pos) {
             q_pos = sq.n_keys - sq.n_new + row / p.group;
             vis = seen(row);
         },
-        [&](bool ok, int s, int r, bool live, float m, float l) {
-            const int row = it.row0 + r;
-            uint16_t *dst = p.out + ((int64_t)(sq.token0 + row / p.group) * p.n_q + it.head0 + row % p.group) * kHeadDim;
-            ta_rows<true>(sm, it, ok, s, live, m, l, [&](int col, const float (&o)[32], float, float) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    reinterpret_cast<uint4 *>(dst + col)[i] =
-                        make_uint4(ta_pack<kHalf>(o[8 * i], o[8 * i + 1]), ta_pack<kHalf>(o[8 * i + 2], o[8 * i + 3]),
-                                   ta_pack<kHalf>(o[8 * i + 4], o[8 * i + 5]), ta_pack<kHalf>(o[8 * i + 6], o[8 * i + 7]));
+        [&](bool ok, int s, bool live, float m, float l) {
+            ta_rows<true>(sm, it, ok, s, live, m, l, [&](int r, int lane, const float4 &o, float, float) {
+                const int row = it.row0 + r;
+                uint16_t *dst = p.out + ((int64_t)(sq.token0 + row / p.group) * p.n_q + it.head0 + row % p.group) * kHeadDim;
+                reinterpret_cast<uint2 *>(dst)[lane] = make_uint2(ta_pack<kHalf>(o.x, o.y), ta_pack<kHalf>(o.z, o.w));
             });
         });
 }
