@@ -505,9 +505,9 @@ __device__ __forceinline__ void ta_block(TaSmem &sm, const TaItem &it, const TaS
     __syncthreads();
     tc_fence_after();
 
-    // registers: 168 a thread at launch; the softmax warps take what the other four leave (8 * 208 + 4 * 80 <= 12 * 168)
+    // registers: 168 a thread at launch; the softmax warps take what the other four leave (8 * 192 + 4 * 120 = 12 * 168)
     if (warp < 8) {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");
         // ---- the queries, then a row of scores per thread ----
         const int tiles = it.shared ? 2 : 1;
 #pragma unroll 4
@@ -530,7 +530,7 @@ __device__ __forceinline__ void ta_block(TaSmem &sm, const TaItem &it, const TaS
         const bool ok = ta_softmax<kHalf, kTwo, kCap, kBias, kCols>(sm, it, sc, s, live, vis, q_pos, slope, key_pos, m, l);
         finish(ok, s, live, m, l);
     } else {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 120;");
         if (warp == 8) {
             // ---- copies ----
             if (ta_elect()) {
@@ -648,77 +648,114 @@ __device__ __forceinline__ void ta_block(TaSmem &sm, const TaItem &it, const TaS
     if (warp == 9) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(sm.tmem), "r"(512));
 }
 
-// O of the rows, out of tensor memory: put(row of the item, lane, its four values of the row, m, l), a row per warp at a time, O times 1 / l
-// (kNormal) or as it is. Parts of one row (the two streams where they take tiles in turn, and its copies in the tile) are joined here. Through
-// shared memory, where the queries and the key and value tiles were, so that a row leaves as one piece of memory. All 256 softmax
-// threads come here, whatever their waits said.
+__device__ __forceinline__ void *ta_shfl(void *p, int lane)
+{
+    const unsigned long long v = reinterpret_cast<unsigned long long>(p);
+    const uint32_t a = __shfl_sync(0xFFFFFFFFu, (uint32_t)v, lane), b = __shfl_sync(0xFFFFFFFFu, (uint32_t)(v >> 32), lane);
+    return reinterpret_cast<void *>((unsigned long long)b << 32 | a);
+}
+
+// O of the rows, out of tensor memory and through shared memory, so that a row leaves in pieces of 256 bytes: fp32 as it is (kOut32) or
+// 16-bit values of O / l. row_at(r) says where row r of the item goes, stats(r, m, l) takes its statistics. All 256 softmax threads
+// come here, whatever their waits said; where one ran out l is NaN, and with it the row.
+// Two row tiles: a warp's 32 rows pass through the warp's own quarter of its stream's queries, which are done with.
+// One: parts of a row (of the two streams, and of its copies in the tile) are joined; each thread scales its own, and they are added
+// up where the key and value tiles were.
 constexpr int kTaPitch = kHeadDim + 4;
 static_assert(2 * kTaTile * kTaPitch * 4 <= kTaRing * kTaTileBytes, "O of both streams fits the ring");
-template <bool kNormal, typename Put>
-__device__ __forceinline__ void ta_rows(TaSmem &sm, const TaItem &it, bool ok, int s, bool live, float m, float l, Put put)
+template <bool kHalf, bool kOut32, typename RowAt, typename Stats>
+__device__ __forceinline__ void ta_rows(TaSmem &sm, const TaItem &it, bool ok, int s, bool live, float m, float l, RowAt row_at, Stats stats)
 {
     const int t = threadIdx.x & 127, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t t_o = sm.tmem + ((uint32_t)(warp & 3) << 21) + 256u + 128u * s;
+    const bool warp_live = __any_sync(0xFFFFFFFFu, live);
+    if (!ok) m = 0.f, l = CUDART_NAN_F;
+    float o[32];
+    if (it.shared) {
+        if (!warp_live) return;
+        const int r0 = kTaTile * s + 32 * (warp & 3), mine = r0 + lane;
+        if (live) stats(mine, m, l);
+        const float by = kOut32 ? (ok ? 1.f : l) : (l == 0.f ? 0.f : __fdividef(1.f, l));
+        void *dst = row_at(min(mine, it.n_rows - 1));
+        unsigned char *stage = sm.q[s] + 8192 * (warp & 3);
+        constexpr int kCols = kOut32 ? 64 : 128;           // columns in 256 bytes
+#pragma unroll
+        for (int pass = 0; pass < kHeadDim / kCols; ++pass) {
+#pragma unroll
+            for (int q = 0; q < kCols / 32; ++q) {
+                ta_ld32(t_o + kCols * pass + 32 * q, o);
+                ta_ld_wait();
+                ta_tie(o);
+#pragma unroll
+                for (int i = 0; i < 32; ++i) o[i] *= by;
+#pragma unroll
+                for (int i = 0; i < (kOut32 ? 8 : 4); ++i) {
+                    const int ch = q * (kOut32 ? 8 : 4) + i;
+                    uint4 x;
+                    if constexpr (kOut32)
+                        x = make_uint4(__float_as_uint(o[4 * i]), __float_as_uint(o[4 * i + 1]), __float_as_uint(o[4 * i + 2]), __float_as_uint(o[4 * i + 3]));
+                    else
+                        x = make_uint4(ta_pack<kHalf>(o[8 * i], o[8 * i + 1]), ta_pack<kHalf>(o[8 * i + 2], o[8 * i + 3]),
+                                       ta_pack<kHalf>(o[8 * i + 4], o[8 * i + 5]), ta_pack<kHalf>(o[8 * i + 6], o[8 * i + 7]));
+                    *reinterpret_cast<uint4 *>(stage + lane * 256 + ((ch ^ (lane & 7)) << 4)) = x;
+                }
+            }
+            __syncwarp();
+#pragma unroll 8
+            for (int i = 0; i < 16; ++i) {
+                const int r = 2 * i + (lane >> 4), ch = lane & 15;
+                uint4 *to = reinterpret_cast<uint4 *>(ta_shfl(dst, r)) + 16 * pass + ch;
+                if (r0 + r < it.n_rows) *to = *reinterpret_cast<const uint4 *>(stage + r * 256 + ((ch ^ (r & 7)) << 4));
+            }
+            __syncwarp();
+        }
+        return;
+    }
     float *rows = reinterpret_cast<float *>(sm.ring[0]);
-    float2 *stat = reinterpret_cast<float2 *>(sm.q[0]);
+    float2 *stat = reinterpret_cast<float2 *>(sm.q[1]);    // (no queries there)
+    const int copy = kTaTile / it.fold, r = t % copy;
+    stat[kTaTile * s + t] = make_float2(m, l);
     ta_named_barrier(1, 256);                              // both streams' products are over
+    float top = -CUDART_INF_F, sum = 0.f;
+    for (int e = r; e < 2 * kTaTile; e += copy) top = fmaxf(top, stat[e].x);
+    const float ref = top == -CUDART_INF_F ? 0.f : top;
+    for (int e = r; e < 2 * kTaTile; e += copy) sum = fmaf(stat[e].y, ta_ex2(stat[e].x - ref), sum);
+    if (live && s == 0 && t < copy) stats(r, top, sum);
     {
-        const uint32_t t_o = sm.tmem + ((uint32_t)(warp & 3) << 21) + 256u + 128u * s;
+        float by = ta_ex2(m - ref);
+        if (sum != sum) by = sum;
+        else if constexpr (!kOut32) by = sum == 0.f ? 0.f : __fdividef(by, sum);
         float *dst = rows + (kTaTile * s + t) * kTaPitch;
-        if ((s ? it.count1 : it.count0) > 0 && __any_sync(0xFFFFFFFFu, live)) {
-            float o[32];
+        if ((s ? it.count1 : it.count0) > 0 && warp_live) {
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 ta_ld32(t_o + 32 * q, o);
                 ta_ld_wait();
                 ta_tie(o);
 #pragma unroll
-                for (int i = 0; i < 32; i += 4) *reinterpret_cast<float4 *>(dst + 32 * q + i) = make_float4(o[i], o[i + 1], o[i + 2], o[i + 3]);
+                for (int i = 0; i < 32; i += 4)
+                    *reinterpret_cast<float4 *>(dst + 32 * q + i) = make_float4(o[i] * by, o[i + 1] * by, o[i + 2] * by, o[i + 3] * by);
             }
         }
-        stat[kTaTile * s + t] = ok ? make_float2(m, l) : make_float2(0.f, CUDART_NAN_F);
     }
     ta_named_barrier(1, 256);
-    const auto leave = [&](int r, float4 x, float top, float sum) {
-        if constexpr (kNormal) {
-            const float by = sum == 0.f ? 0.f : __fdividef(1.f, sum);
-            x.x *= by;
-            x.y *= by;
-            x.z *= by;
-            x.w *= by;
-        }
-        put(r, lane, x, top, sum);
-    };
-    if (it.shared) {
+    const int streams = it.count1 > 0 ? 2 : 1;             // (a stream without a tile has left nothing)
+    void *dst = row_at(min(8 * (lane & 15) + warp, it.n_rows - 1));
 #pragma unroll 4
-        for (int i = 0; i < kTaTile / 4; ++i) {
-            const int r = 8 * i + warp;
-            if (r >= it.n_rows) continue;
-            const float2 st = stat[r];
-            leave(r, st.y != st.y ? make_float4(st.y, st.y, st.y, st.y) : reinterpret_cast<const float4 *>(rows + r * kTaPitch)[lane], st.x, st.y);
-        }
-        return;
-    }
-    const int copy = kTaTile / it.fold;
-#pragma unroll 2
     for (int i = 0; i < kTaTile / 8; ++i) {
-        const int r = 8 * i + warp;
-        if (r >= it.n_rows) continue;
-        float top = -CUDART_INF_F, sum = 0.f;
-        for (int e = r; e < 2 * kTaTile; e += copy) top = fmaxf(top, stat[e].x);
-        const float ref = top == -CUDART_INF_F ? 0.f : top;
+        const int row = 8 * i + warp;
+        void *to = ta_shfl(dst, i);
+        if (row >= it.n_rows) break;
         float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int e = r; e < 2 * kTaTile; e += copy) {
-            const float2 st = stat[e];
-            if (st.y == 0.f) continue;                     // (no key seen; where a stream has no tile, nothing was written)
-            const float w = st.y != st.y ? st.y : ta_ex2(st.x - ref);
+        for (int e = row; e < streams * kTaTile; e += copy) {
             const float4 y = reinterpret_cast<const float4 *>(rows + e * kTaPitch)[lane];
-            sum = fmaf(w, st.y, sum);
-            x.x = fmaf(w, y.x, x.x);
-            x.y = fmaf(w, y.y, x.y);
-            x.z = fmaf(w, y.z, x.z);
-            x.w = fmaf(w, y.w, x.w);
+            x.x += y.x;
+            x.y += y.y;
+            x.z += y.z;
+            x.w += y.w;
         }
-        leave(r, x, top, sum);
+        if constexpr (kOut32) reinterpret_cast<float4 *>(to)[lane] = x;
+        else                  reinterpret_cast<uint2 *>(to)[lane] = make_uint2(ta_pack<kHalf>(x.x, x.y), ta_pack<kHalf>(x.z, x.w));
     }
 }
 

@@ -81,11 +81,10 @@ prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__
             if (kBias) q_pos = p.n_keys + suffix_rows(p, row / p.group) - 1;
         },
         [&](bool ok, int s, bool live, float m, float l) {
-            ta_rows<false>(sm, it, ok, s, live, m, l, [&](int r, int lane, const float4 &o, float top, float sum) {
-                const int64_t slot = ((int64_t)j * p.parts + part) * p.rows + it.row0 + r;
-                reinterpret_cast<float4 *>(p.part_o + slot * kHeadDim)[lane] = o;
-                if (lane == 0) p.part_ml[slot] = make_float2(top, sum);
-            });
+            const int64_t slot = ((int64_t)j * p.parts + part) * p.rows + it.row0;
+            ta_rows<kHalf, true>(
+                sm, it, ok, s, live, m, l, [&](int r) { return static_cast<void *>(p.part_o + (slot + r) * kHeadDim); },
+                [&](int r, float top, float sum) { p.part_ml[slot + r] = make_float2(top, sum); });
         });
 }
 

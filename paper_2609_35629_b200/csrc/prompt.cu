@@ -75,11 +75,13 @@ prompt_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__
             vis = seen(row);
         },
         [&](bool ok, int s, bool live, float m, float l) {
-            ta_rows<true>(sm, it, ok, s, live, m, l, [&](int r, int lane, const float4 &o, float, float) {
-                const int row = it.row0 + r;
-                uint16_t *dst = p.out + ((int64_t)(sq.token0 + row / p.group) * p.n_q + it.head0 + row % p.group) * kHeadDim;
-                reinterpret_cast<uint2 *>(dst)[lane] = make_uint2(ta_pack<kHalf>(o.x, o.y), ta_pack<kHalf>(o.z, o.w));
-            });
+            ta_rows<kHalf, false>(
+                sm, it, ok, s, live, m, l,
+                [&](int r) {
+                    const int row = it.row0 + r;
+                    return static_cast<void *>(p.out + ((int64_t)(sq.token0 + row / p.group) * p.n_q + it.head0 + row % p.group) * kHeadDim);
+                },
+                [](int, float, float) {});
         });
 }
 
