@@ -43,7 +43,7 @@ constexpr int kTaPolyEvery = 4;           // of so many pairs of exponentials on
 struct TaSmem {
     alignas(1024) unsigned char q[2][kTaTileBytes];
     unsigned char ring[kTaRing][kTaTileBytes];
-    uint64_t full[kTaRing], empty[kTaRing];   // a tile has landed; the products have left it
+    uint64_t full[4], left[4];                // a group of tiles has landed; the products have left it. By group % 4
     uint64_t q_ready, s_ready[2], p_ready[2][2], done[2];      // p_ready: weights of keys 0-95, 96-127
     uint64_t pos_ready[2][2], tail;           // tail: the last tile of values has landed, with somebody else's rows behind it
     alignas(16) float pos[2][2][kTaTile];                 // positions of the keys of a stream's tile, less n_keys; by tile parity
@@ -257,14 +257,17 @@ __device__ __forceinline__ void ta_ex2_poly(uint64_t x, float &a, float &b)
 }
 
 template <int kStream> struct TaStream { static constexpr int value = kStream; };
-// Place of a tile in the order in which the ring is filled, which is that of first use: K_0 V_0 K_1 V_1 ... where both streams use
-// a tile, K_0 K_1 V_0 K_2 V_1 K_3 ... where they take tiles in turn. Slot: place % kTaRing.
+// The ring is filled in the order of first use, and in groups that land and are left together (a wait and a commit each, which cost the
+// issuing lane a hundred or two hundred cycles apiece): where both streams use a tile, K_0 | V_0 K_1 | V_1 K_2 | ..., where they take
+// tiles in turn, K_0 K_1 | V_0 K_2 | V_1 K_3 | ... Slot: place % kTaRing.
 __device__ __forceinline__ int ta_tiles(const TaItem &it) { return it.shared ? it.count1 : it.count0 + it.count1; }
 __device__ __forceinline__ int ta_key_place(const TaItem &it, int tile) { return it.shared ? 2 * tile : max(2 * tile - 1, 0); }
 __device__ __forceinline__ int ta_value_place(const TaItem &it, int tile)
 {
     return it.shared ? 2 * tile + 1 : min(2 * tile + 2, 2 * ta_tiles(it) - 1);
 }
+// (of a place that is not the last)
+__device__ __forceinline__ int ta_group(const TaItem &it, int place) { return it.shared ? (place + 1) / 2 : place / 2; }
 __device__ __forceinline__ bool ta_cut(const TaItem &it) { return it.fix_tail && it.n_keys < (it.tile0 + ta_tiles(it)) * kTaTile; }
 
 // cap * tanh(x cap_in) * log2 e of a thread's products. |x cap_in| <= 1 throughout the warp, the usual case: tanh(y) = y P(y^2), P with the
@@ -483,9 +486,9 @@ __device__ __forceinline__ void ta_block(TaSmem &sm, const TaItem &it, const TaS
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     if (tid == 0) {
         sm.failed = 0;
-        for (int i = 0; i < kTaRing; ++i) {
-            asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(ta_addr(&sm.full[i])), "r"(1));
-            asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(ta_addr(&sm.empty[i])), "r"(1));
+        for (int i = 0; i < 4; ++i) {
+            asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(ta_addr(&sm.full[i])), "r"(2));
+            asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(ta_addr(&sm.left[i])), "r"(1));
         }
         asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(ta_addr(&sm.q_ready)), "r"(256));
         asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(ta_addr(&sm.tail)), "r"(1));
@@ -534,14 +537,17 @@ __device__ __forceinline__ void ta_block(TaSmem &sm, const TaItem &it, const TaS
         if (warp == 8) {
             // ---- copies ----
             if (ta_elect()) {
-                int n = 0;                                 // tiles asked for
+                int n = 0, waited = -1;                    // tiles asked for; the last group known to be left
                 const int n_tiles = ta_tiles(it);
                 const bool cut = ta_cut(it);
-                const auto ask = [&](bool value, int tile) {
-                    const int slot = n % kTaRing;
-                    if (n >= kTaRing && !ta_wait(sm, &sm.empty[slot], (uint32_t)(n / kTaRing - 1) & 1u)) return false;
+                const auto ask = [&](bool value, int tile, int group) {
+                    if (n >= kTaRing) {
+                        const int g = ta_group(it, n - kTaRing);
+                        if (g > waited && !ta_wait(sm, &sm.left[g & 3], (uint32_t)(g >> 2) & 1u)) return false;
+                        waited = g;
+                    }
                     // (warp 10 hands on a tile of values that ends in somebody else's rows)
-                    const uint32_t bar = ta_addr(value && cut && tile == n_tiles - 1 ? &sm.tail : &sm.full[slot]), dst = ta_addr(sm.ring[slot]);
+                    const uint32_t bar = ta_addr(value && cut && tile == n_tiles - 1 ? &sm.tail : &sm.full[group & 3]), dst = ta_addr(sm.ring[n % kTaRing]);
                     const int y = it.key0 + (it.tile0 + tile) * kTaTile;
                     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(kTaTileBytes) : "memory");
                     const CUtensorMap *map = value ? v_map : k_map;
@@ -550,21 +556,27 @@ __device__ __forceinline__ void ta_block(TaSmem &sm, const TaItem &it, const TaS
                     ++n;
                     return true;
                 };
-                bool ok = true;
-                if (!it.shared) ok = ask(false, 0);
+                const auto alone = [&](int group) { mbar_arrive(ta_addr(&sm.full[group & 3])); };      // a group of one tile
+                const int ahead = it.shared ? 1 : 2;       // keys are so many tiles ahead of the values
+                int groups = 0;
+                bool ok = ask(false, 0, 0);
+                if (ok && ahead == 2 && n_tiles > 1) ok = ask(false, 1, 0);
+                else alone(0);
                 for (int i = 0; ok && i < n_tiles; ++i) {
-                    const int keys = it.shared ? i : i + 1;
-                    if (keys < n_tiles) ok = ask(false, keys);
-                    ok = ok && ask(true, i);
+                    groups = i + 1;
+                    ok = ask(true, i, groups);
+                    if (ok && i + ahead < n_tiles) ok = ask(false, i + ahead, groups);
+                    else if (ok) alone(groups);
                 }
                 // nothing leaves while a copy is under way (in the normal course the products have waited for all of them)
-                for (int i = max(0, n - kTaRing); i < n; ++i) tc_wait(ta_addr(&sm.full[i % kTaRing]), (uint32_t)(i / kTaRing) & 1u);
+                if (!ok)
+                    for (int g = max(0, groups - 3); g <= groups; ++g) tc_wait(ta_addr(&sm.full[g & 3]), (uint32_t)(g >> 2) & 1u);
             }
             __syncwarp();
         } else if (warp == 9) {
             // ---- products: one lane. Strictly in turn, stream 0's weights with its values and its next scores, then stream 1's: when both
             // streams' weights are there at once, one still gets its scores a thousand cycles before the other, and its exponentials
-            // are taken while the other's products run (a warp per stream left both waiting for one another's halves: 515 us for 481) ----
+            // are taken while the other's products run (a warp per stream left both waiting for one another's halves: 515 us for 442) ----
             const uint32_t tmem = __shfl_sync(0xFFFFFFFFu, sm.tmem, 0);
             if (ta_elect()) {
                 const uint32_t idesc_s = tc_idesc(kTaTile, kTaTile, 0, 0, kHalf), idesc_o = tc_idesc(kTaTile, kHeadDim, 0, 1, kHalf);
@@ -572,28 +584,22 @@ __device__ __forceinline__ void ta_block(TaSmem &sm, const TaItem &it, const TaS
                 const uint32_t q_low = (uint32_t)tc_desc_sw128(ta_addr(sm.q[0]), 16, 1024), k_low = (uint32_t)tc_desc_sw128(ta_addr(sm.ring[0]), 16, 1024);
                 const uint32_t v_low = (uint32_t)tc_desc_sw128(ta_addr(sm.ring[0]), kTaTileBytes / 2, 1024), upper = (uint32_t)(tc_desc_sw128(0, 16, 1024) >> 32);
                 const uint32_t q1_low = q_low + (it.shared ? kTaTileBytes >> 4 : 0);
-                const auto landed = [&](int place) { return ta_wait(sm, &sm.full[place % kTaRing], (uint32_t)(place / kTaRing) & 1u); };
-                // a tile's last use of the two: what was issued so far over, its slot is free
-                const auto leave = [&](int s, int c, int place) {
-                    if (s == 1 || !it.shared || c >= it.count1) tc_commit(ta_addr(&sm.empty[place % kTaRing]));
-                };
-                const auto scores = [&](auto stream, int c) {
+                const int n_tiles = ta_tiles(it);
+                const auto landed = [&](int g) { return ta_wait(sm, &sm.full[g & 3], (uint32_t)(g >> 2) & 1u); };
+                const auto scores = [&](auto stream, int tile) {
                     constexpr int s = decltype(stream)::value;
-                    const int place = ta_key_place(it, it.shared ? c : 2 * c + s);
-                    const uint32_t a = s ? q1_low : q_low, b = k_low + (uint32_t)(place % kTaRing * (kTaTileBytes >> 4));
+                    const uint32_t a = s ? q1_low : q_low, b = k_low + (uint32_t)(ta_key_place(it, tile) % kTaRing * (kTaTileBytes >> 4));
 #pragma unroll
                     for (int x = 0; x < 8; ++x) {
                         const uint32_t at = ((x >> 2) * (kTaTileBytes / 2) + (x & 3) * 32) >> 4;
                         ta_mma_ss(tmem + 128u * s, a + at, b + at, upper, idesc_s, x > 0 ? 1u : 0u);
                     }
                     tc_commit(ta_addr(&sm.s_ready[s]));
-                    leave(s, c, place);
                 };
-                const auto values = [&](auto stream, int c) {
+                // the stream's c-th tile of weights
+                const auto values = [&](auto stream, int c, int tile) {
                     constexpr int s = decltype(stream)::value;
-                    const int count = s ? it.count1 : it.count0, tile = it.shared ? c : 2 * c + s, place = ta_value_place(it, tile);
-                    const uint32_t b = v_low + (uint32_t)(place % kTaRing * (kTaTileBytes >> 4));
-                    if (!landed(place)) return false;
+                    const uint32_t b = v_low + (uint32_t)(ta_value_place(it, tile) % kTaRing * (kTaTileBytes >> 4));
 #pragma unroll
                     for (int part = 0; part < 2; ++part) {                  // keys 0 .. 95, 96 .. 127
                         if (!ta_wait(sm, &sm.p_ready[s][part], c & 1)) return false;
@@ -604,26 +610,34 @@ __device__ __forceinline__ void ta_block(TaSmem &sm, const TaItem &it, const TaS
                             for (int term = 0; term < (kTwo ? 2 : 1); ++term)
                                 ta_mma_ts(tmem + 256u + 128u * s, tmem + 128u * s + 64u * term + 8u * x, b + ((x * 2048) >> 4), upper, idesc_o,
                                           x > 0 || term > 0 ? 1u : (c > 0 ? 1u : 0u));
-                        // (the keys of the product behind this one)
-                        if (part == 0 && c + 1 < count && !landed(ta_key_place(it, it.shared ? c + 1 : 2 * c + 2 + s))) return false;
                     }
-                    if (c + 1 == count) tc_commit(ta_addr(&sm.done[s]));
-                    leave(s, c, place);
-                    if (c + 1 < count) scores(stream, c + 1);
+                    if (c + 1 == (s ? it.count1 : it.count0)) tc_commit(ta_addr(&sm.done[s]));
                     return true;
                 };
-                bool ok = ta_wait(sm, &sm.q_ready, 0);
-                if (ok && it.count0 > 0 && (ok = landed(0))) {
+                bool ok = ta_wait(sm, &sm.q_ready, 0) && landed(0);
+                if (ok) {
                     tc_fence_after();
                     scores(TaStream<0>{}, 0);
+                    if (it.count1 > 0) scores(TaStream<1>{}, it.shared ? 0 : 1);
+                    tc_commit(ta_addr(&sm.left[0]));
                 }
-                if (ok && it.count1 > 0 && (ok = landed(ta_key_place(it, it.shared ? 0 : 1)))) {
-                    tc_fence_after();
-                    scores(TaStream<1>{}, 0);
-                }
-                for (int c = 0; ok && c < max(it.count0, it.count1); ++c) {
-                    if (c < it.count0) ok = values(TaStream<0>{}, c);
-                    if (ok && c < it.count1) ok = values(TaStream<1>{}, c);
+                const int rounds = it.shared ? n_tiles : it.count0;
+                for (int c = 0; ok && c < rounds; ++c) {
+                    const int t0 = it.shared ? c : 2 * c, t1 = it.shared ? c : 2 * c + 1, step = it.shared ? 1 : 2;
+                    if (!(ok = landed(t0 + 1))) break;
+                    if (c < it.count0) {
+                        if (!(ok = values(TaStream<0>{}, c, t0))) break;
+                        if (c + 1 < it.count0) scores(TaStream<0>{}, t0 + step);
+                    }
+                    if (!it.shared) {
+                        tc_commit(ta_addr(&sm.left[(t0 + 1) & 3]));
+                        if (c < it.count1 && !(ok = landed(t1 + 1))) break;
+                    }
+                    if (c < it.count1) {
+                        if (!(ok = values(TaStream<1>{}, c, t1))) break;
+                        if (c + 1 < it.count1) scores(TaStream<1>{}, t1 + step);
+                        tc_commit(ta_addr(&sm.left[(t1 + 1) & 3]));
+                    }
                 }
                 if (!ok) {                                 // products under way finish before their memory goes
                     for (int i = 0; i < 4096; ++i) __nanosleep(256);
@@ -638,7 +652,7 @@ __device__ __forceinline__ void ta_block(TaSmem &sm, const TaItem &it, const TaS
                 for (int e = max(valid, 0) * 16 + lane; e < kTaTile * 16; e += 32)
                     *reinterpret_cast<uint4 *>(sm.ring[place % kTaRing] + ta_byte(e >> 4, e & 15)) = make_uint4(0, 0, 0, 0);
                 proxy_fence();
-                ta_arrive_warp(&sm.full[place % kTaRing]);
+                ta_arrive_warp(&sm.full[ta_tiles(it) & 3]);          // (the last group is this tile's)
             }
         }
     }
