@@ -613,27 +613,43 @@ def _refuse(why):
     raise SantappError(SANTAPP_ERR_INVALID_ARG, why)
 
 
-def _expect(name, t, shape, dtype, dense=True):
-    """The address of a tensor of exactly this shape and type on the current device (None in `shape`: any size). Not
-    dense: the first dimension may have any stride."""
-    if not t.is_cuda or t.get_device() != torch._C._cuda_getDevice():
+def _device():
+    """The current device's index, which no tensor has where there is none."""
+    try:
+        return torch._C._cuda_getDevice()
+    except RuntimeError:
+        return -2
+
+
+def _wrong(name, t, shape, dtype, dense):
+    if not t.is_cuda or t.get_device() != _device():
         _refuse(f"{name} must be a CUDA tensor on the current device")
     if t.dtype != dtype:
         _refuse(f"{name} must be {dtype}")
-    if len(t.shape) != len(shape) or any(want is not None and have != want for have, want in zip(t.shape, shape)):
+    if t.shape != shape:
         _refuse(f"{name} must have the shape {list(shape)}, not {list(t.shape)}")
-    if not (t.is_contiguous() if dense or t.shape[0] == 0 else t[0].is_contiguous()):
-        _refuse(f"{name} must be contiguous" + ("" if dense else " behind its first dimension"))
+    _refuse(f"{name} must be contiguous" + ("" if dense else " behind its first dimension"))
+
+
+def _expect(name, t, shape, dtype, device):
+    """The address of a dense tensor of this shape and type on this device."""
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != device or not t.is_contiguous():
+        _wrong(name, t, shape, dtype, True)
     return t.data_ptr()
 
 
-def _expect_or_none(name, t, shape, dtype):
-    return None if t is None else _expect(name, t, shape, dtype)
+def _expect_planes(name, t, shape, dtype, device):
+    """The same where the first dimension may have any stride: address and stride (of one plane: what a dense tensor has)."""
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != device:
+        _wrong(name, t, shape, dtype, False)
+    steps, plane = t.stride(), shape[1] * shape[2] if len(shape) == 3 else shape[1]
+    if steps[1:] != ((shape[2], 1) if len(shape) == 3 else (1,)) and plane and not t[0].is_contiguous():
+        _wrong(name, t, shape, dtype, False)
+    return t.data_ptr(), steps[0] if shape[0] > 1 else plane
 
 
-def _token_stride(t):
-    """Elements from token to token (of one token: what a dense tensor would have)."""
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
+def _expect_or_none(name, t, shape, dtype, device):
+    return None if t is None else _expect(name, t, shape, dtype, device)
 
 
 class Rope:
@@ -650,20 +666,20 @@ class Rope:
             if len(values) != rot_dim // 2 or rot_dim > 128:
                 _refuse("inv_freq holds rot_dim / 2 values")
             self.c.inv_freq[:len(values)] = values
+        self.ref = ctypes.byref(self.c)
 
     @property
     def inv_freq(self):
         return list(self.c.inv_freq[:self.c.rot_dim // 2])
 
 
-def _rope_rows(geom, n, q, k, v, q_out):
-    d, dt = geom.head_dim, geom.torch_dtype
+def _rope_rows(geom, n, q, k, v, q_out, device):
+    d, kv, dt = geom.head_dim, geom.n_kv_heads, geom.torch_dtype
+    heads, keys = (n, geom.n_q_heads, d), (n, kv, d)
     if q_out is None:
-        q_out = torch.empty((n, geom.n_q_heads, d), dtype=dt, device=q.device)
-    return q_out, [_expect("q", q, (n, geom.n_q_heads, d), dt, False), _token_stride(q),
-                   _expect("k", k, (n, geom.n_kv_heads, d), dt, False), _token_stride(k),
-                   _expect("v", v, (n, geom.n_kv_heads, d), dt, False), _token_stride(v)], \
-        _expect("q_out", q_out, (n, geom.n_q_heads, d), dt)
+        q_out = torch.empty(heads, dtype=dt, device=q.device)
+    return (q_out, *_expect_planes("q", q, heads, dt, device), *_expect_planes("k", k, keys, dt, device),
+            *_expect_planes("v", v, keys, dt, device), _expect("q_out", q_out, heads, dt, device))
 
 
 def santapp_rope_append(geom: Geometry, rope: Rope, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
@@ -672,14 +688,15 @@ def santapp_rope_append(geom: Geometry, rope: Rope, q: torch.Tensor, k: torch.Te
                         stream=None) -> torch.Tensor:
     """q [B, Hq, d], k and v [B, Hkv, d] (any stride between tokens); base_pos, suffix_len int32 [B]; k_suffix, v_suffix
     [B, Hkv, cap, d]. Row suffix_len[b] is written, q_out returned; suffix_len_out (may be suffix_len) gets suffix_len + 1."""
-    L = load_library()
-    B = geom.n_seqs
-    q_out, rows, q_dst = _rope_rows(geom, B, q, k, v, q_out)
-    shape = (B, geom.n_kv_heads, None, geom.head_dim)
-    ks, vs = _expect("k_suffix", k_suffix, shape, geom.torch_dtype), _expect("v_suffix", v_suffix, tuple(k_suffix.shape), geom.torch_dtype)
-    _check(L.santapp_rope_append(geom.ref(), ctypes.byref(rope.c), *rows, _expect("base_pos", base_pos, (B,), torch.int32),
-                                 _expect("suffix_len", suffix_len, (B,), torch.int32), q_dst, ks, vs, k_suffix.shape[2],
-                                 _expect_or_none("suffix_len_out", suffix_len_out, (B,), torch.int32), _stream_ptr(stream)))
+    B, dt, i32, dev = geom.n_seqs, geom.torch_dtype, torch.int32, _device()
+    q_out, qp, qs, kp, ks, vp, vs, dst = _rope_rows(geom, B, q, k, v, q_out, dev)
+    cap, one = k_suffix.shape[2], (B,)
+    shape = (B, geom.n_kv_heads, cap, geom.head_dim)
+    _check(load_library().santapp_rope_append(
+        geom.ref(), rope.ref, qp, qs, kp, ks, vp, vs, _expect("base_pos", base_pos, one, i32, dev),
+        _expect("suffix_len", suffix_len, one, i32, dev), dst, _expect("k_suffix", k_suffix, shape, dt, dev),
+        _expect("v_suffix", v_suffix, shape, dt, dev), cap, _expect_or_none("suffix_len_out", suffix_len_out, one, i32, dev),
+        _stream_ptr(stream)))
     return q_out
 
 
@@ -689,15 +706,14 @@ def santapp_rope_prompt(geom: Geometry, rope: Rope, q: torch.Tensor, k: torch.Te
                         stream=None) -> torch.Tensor:
     """q [n, Hq, d], k and v [n, Hkv, d] (any stride between tokens); positions, dst_row int32 [n] or None (the row's
     index); k_prompt, v_prompt [Hkv, rows, d], written at dst_row. Returns q_out [n, Hq, d]."""
-    L = load_library()
-    n = q.shape[0]
-    q_out, rows, q_dst = _rope_rows(geom, n, q, k, v, q_out)
-    shape = (geom.n_kv_heads, None, geom.head_dim)
-    kp, vp = _expect("k_prompt", k_prompt, shape, geom.torch_dtype), _expect("v_prompt", v_prompt, tuple(k_prompt.shape), geom.torch_dtype)
-    _check(L.santapp_rope_prompt(geom.ref(), ctypes.byref(rope.c), n, *rows,
-                                 _expect_or_none("positions", positions, (n,), torch.int32),
-                                 _expect_or_none("dst_row", dst_row, (n,), torch.int32), q_dst, kp, vp, k_prompt.shape[1],
-                                 _stream_ptr(stream)))
+    n, dt, i32, dev = q.shape[0], geom.torch_dtype, torch.int32, _device()
+    q_out, qp, qs, kp, ks, vp, vs, dst = _rope_rows(geom, n, q, k, v, q_out, dev)
+    rows = k_prompt.shape[1]
+    shape = (geom.n_kv_heads, rows, geom.head_dim)
+    _check(load_library().santapp_rope_prompt(
+        geom.ref(), rope.ref, n, qp, qs, kp, ks, vp, vs, _expect_or_none("positions", positions, (n,), i32, dev),
+        _expect_or_none("dst_row", dst_row, (n,), i32, dev), dst, _expect("k_prompt", k_prompt, shape, dt, dev),
+        _expect("v_prompt", v_prompt, shape, dt, dev), rows, _stream_ptr(stream)))
     return q_out
 
 
@@ -705,22 +721,22 @@ def santapp_suffix_fork(geom: Geometry, src: torch.Tensor, suffix_len: torch.Ten
                         v_suffix: torch.Tensor, suffix_len_out: Optional[torch.Tensor] = None, stream=None) -> None:
     """Slot b of k_suffix / v_suffix [B, Hkv, cap, d] continues slot src[b] (int32 [B]; outside [0, B): freed), in place;
     suffix_len_out (not suffix_len) gets the new lengths."""
-    L = load_library()
-    B = geom.n_seqs
-    shape = (B, geom.n_kv_heads, None, geom.head_dim)
-    ks, vs = _expect("k_suffix", k_suffix, shape, geom.torch_dtype), _expect("v_suffix", v_suffix, tuple(k_suffix.shape), geom.torch_dtype)
-    _check(L.santapp_suffix_fork(geom.ref(), _expect("src", src, (B,), torch.int32),
-                                 _expect("suffix_len", suffix_len, (B,), torch.int32), ks, vs, k_suffix.shape[2],
-                                 _expect_or_none("suffix_len_out", suffix_len_out, (B,), torch.int32), _stream_ptr(stream)))
+    B, dt, i32, dev = geom.n_seqs, geom.torch_dtype, torch.int32, _device()
+    cap, one = k_suffix.shape[2], (B,)
+    shape = (B, geom.n_kv_heads, cap, geom.head_dim)
+    _check(load_library().santapp_suffix_fork(
+        geom.ref(), _expect("src", src, one, i32, dev), _expect("suffix_len", suffix_len, one, i32, dev),
+        _expect("k_suffix", k_suffix, shape, dt, dev), _expect("v_suffix", v_suffix, shape, dt, dev), cap,
+        _expect_or_none("suffix_len_out", suffix_len_out, one, i32, dev), _stream_ptr(stream)))
 
 
 def santapp_prefix_decode_workspace_bytes(geom: Geometry, prefix_len: int, suffix_cap: int) -> int:
     return int(load_library().santapp_prefix_decode_workspace_bytes(geom.ref(), prefix_len, suffix_cap))
 
 
-def _attn_opts(geom, scale, cap, slopes, status):
-    return CAttnOpts(scale, cap, _expect_or_none("slopes", slopes, (geom.n_q_heads,), torch.float32),
-                     _expect_or_none("status", status, (1,), torch.int32))
+def _attn_opts(geom, scale, cap, slopes, status, device):
+    return CAttnOpts(scale, cap, _expect_or_none("slopes", slopes, (geom.n_q_heads,), torch.float32, device),
+                     _expect_or_none("status", status, (1,), torch.int32, device))
 
 
 def santapp_prefix_decode_attn(geom: Geometry, k_prefix: Optional[torch.Tensor], v_prefix: Optional[torch.Tensor],
@@ -731,37 +747,36 @@ def santapp_prefix_decode_attn(geom: Geometry, k_prefix: Optional[torch.Tensor],
                                status: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """One prompt for the whole batch: k_prefix, v_prefix [Hkv, N, d] (the planes may lie further apart; None: no prompt),
     prefix_token int32 of the same planes or None; q [B, Hq, d]; suffix as in santapp_decode_attn. fp32 [B, Hq, d]."""
-    L = load_library()
-    B, kv, d, dt = geom.n_seqs, geom.n_kv_heads, geom.head_dim, geom.torch_dtype
-    n = plane = 0
-    kp = vp = tok = None
+    B, kv, d, dt, dev = geom.n_seqs, geom.n_kv_heads, geom.head_dim, geom.torch_dtype, _device()
+    heads = (B, geom.n_q_heads, d)
+    n = plane = suffix_cap = 0
+    kp = vp = tok = ks = vs = None
     if k_prefix is not None:
         n = k_prefix.shape[1]
-        kp = _expect("k_prefix", k_prefix, (kv, None, d), dt, False)
-        vp = _expect("v_prefix", v_prefix, (kv, n, d), dt, False)
-        plane = k_prefix.stride(0) // d if kv > 1 else n
-        if kv > 1 and (k_prefix.stride(0) % d or v_prefix.stride(0) != k_prefix.stride(0)):
+        kp, apart = _expect_planes("k_prefix", k_prefix, (kv, n, d), dt, dev)
+        vp, v_apart = _expect_planes("v_prefix", v_prefix, (kv, n, d), dt, dev)
+        plane = apart // d
+        if apart % d or v_apart != apart:
             _refuse("the planes of k_prefix and v_prefix must lie whole rows and equally far apart")
         if prefix_token is not None:
-            tok = _expect("prefix_token", prefix_token, (kv, n), torch.int32, False)
-            if kv > 1 and prefix_token.stride(0) != plane:
+            tok, t_apart = _expect_planes("prefix_token", prefix_token, (kv, n), torch.int32, dev)
+            if t_apart != plane:
                 _refuse("the planes of prefix_token must lie as far apart as those of k_prefix")
-    ks = vs = None
-    suffix_cap = 0
     if k_suffix is not None:
         suffix_cap = k_suffix.shape[2]
-        ks = _expect("k_suffix", k_suffix, (B, kv, None, d), dt)
-        vs = _expect("v_suffix", v_suffix, (B, kv, suffix_cap, d), dt)
+        ks = _expect("k_suffix", k_suffix, (B, kv, suffix_cap, d), dt, dev)
+        vs = _expect("v_suffix", v_suffix, (B, kv, suffix_cap, d), dt, dev)
     if out is None:
-        out = torch.empty((B, geom.n_q_heads, d), dtype=torch.float32, device=q.device)
+        out = torch.empty(heads, dtype=torch.float32, device=q.device)
     if workspace is None:
         workspace = torch.empty(santapp_prefix_decode_workspace_bytes(geom, n, suffix_cap), dtype=torch.uint8, device=q.device)
-    o = _attn_opts(geom, scale, cap, slopes, status)
-    _check(L.santapp_prefix_decode_attn(geom.ref(), kp, vp, n, plane, tok, _expect("q", q, (B, geom.n_q_heads, d), dt), ks, vs,
-                                        _expect_or_none("suffix_len", suffix_len, (B,), torch.int32), suffix_cap,
-                                        ctypes.byref(o), _expect("out", out, (B, geom.n_q_heads, d), torch.float32),
-                                        _expect("workspace", workspace, (None,), torch.uint8), workspace.numel(),
-                                        _stream_ptr(stream)))
+    size = workspace.numel()
+    o = _attn_opts(geom, scale, cap, slopes, status, dev)
+    _check(load_library().santapp_prefix_decode_attn(
+        geom.ref(), kp, vp, n, plane, tok, _expect("q", q, heads, dt, dev), ks, vs,
+        _expect_or_none("suffix_len", suffix_len, (B,), torch.int32, dev), suffix_cap, ctypes.byref(o),
+        _expect("out", out, heads, torch.float32, dev), _expect("workspace", workspace, (size,), torch.uint8, dev), size,
+        _stream_ptr(stream)))
     return out
 
 
@@ -771,21 +786,21 @@ def santapp_prompt_attn(geom: Geometry, prompt_len, q: torch.Tensor, k_prompt: t
                         status: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """q [sum(new_len or prompt_len), Hq, d]: the last new_len rows of each sequence; k_prompt, v_prompt
     [Hkv, sum(prompt_len), d]. Returns the element type, shaped like q."""
-    L = load_library()
     if len(prompt_len) != geom.n_seqs or any(x is not None and len(x) != geom.n_seqs for x in (new_len, prefix_len)):
         _refuse("prompt_len, new_len and prefix_len hold a length per sequence")
-    n, keys, d, dt = sum(prompt_len if new_len is None else new_len), sum(prompt_len), geom.head_dim, geom.torch_dtype
+    dt, dev = geom.torch_dtype, _device()
+    heads, keys = (sum(prompt_len if new_len is None else new_len), geom.n_q_heads, geom.head_dim), \
+        (geom.n_kv_heads, sum(prompt_len), geom.head_dim)
     if out is None:
-        out = torch.empty((n, geom.n_q_heads, d), dtype=dt, device=q.device)
-    if n == 0:
+        out = torch.empty(heads, dtype=dt, device=q.device)
+    if heads[0] == 0:
         return out
-    o = _attn_opts(geom, scale, cap, slopes, status)
-    _check(L.santapp_prompt_attn(geom.ref(), _i32_array(prompt_len), None if new_len is None else _i32_array(new_len),
-                                 None if prefix_len is None else _i32_array(prefix_len),
-                                 _expect("q", q, (n, geom.n_q_heads, d), dt),
-                                 _expect("k_prompt", k_prompt, (geom.n_kv_heads, keys, d), dt),
-                                 _expect("v_prompt", v_prompt, (geom.n_kv_heads, keys, d), dt), ctypes.byref(o),
-                                 _expect("out", out, (n, geom.n_q_heads, d), dt), _stream_ptr(stream)))
+    o = _attn_opts(geom, scale, cap, slopes, status, dev)
+    _check(load_library().santapp_prompt_attn(
+        geom.ref(), _i32_array(prompt_len), None if new_len is None else _i32_array(new_len),
+        None if prefix_len is None else _i32_array(prefix_len), _expect("q", q, heads, dt, dev),
+        _expect("k_prompt", k_prompt, keys, dt, dev), _expect("v_prompt", v_prompt, keys, dt, dev), ctypes.byref(o),
+        _expect("out", out, heads, dt, dev), _stream_ptr(stream)))
     return out
 
 

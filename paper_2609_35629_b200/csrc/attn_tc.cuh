@@ -38,7 +38,6 @@ constexpr int kTaTile = 128;              // query rows of a stream, keys of a t
 constexpr int kTaTileBytes = kTaTile * kHeadDim * 2;
 constexpr int kTaRing = 5;                // tiles of keys or values under way
 constexpr float kTaSlack = 8.f;
-constexpr int kTaPolyEvery = 4;           // of so many pairs of exponentials one is computed by a polynomial
 
 struct TaSmem {
     alignas(1024) unsigned char q[2][kTaTileBytes];
@@ -53,10 +52,15 @@ struct TaSmem {
 constexpr int kTaSmemBytes = sizeof(TaSmem);
 static_assert(kTaSmemBytes <= 227 * 1024, "shared memory budget");
 
+// row / group and row % group for rows below 2^29 and groups up to 8: by_group is 2^32 / group rounded up to a whole number above it
+__host__ __device__ __forceinline__ uint32_t ta_by_group(int group) { return group == 1 ? 0u : (uint32_t)((0x100000000ull) / (uint32_t)group) + 1u; }
+__device__ __forceinline__ int ta_token(int row, uint32_t by_group) { return by_group ? (int)__umulhi((uint32_t)row, by_group) : row; }
+
 // What a block works on.
 struct TaItem {
     int head0;                // first query head of the KV head
     int group, n_q;
+    uint32_t by_group;        // ta_by_group(group)
     const uint16_t *q;        // row r is q + ((r / group) * n_q + head0 + r % group) * 128
     int n_rows;               // query rows from r = row0 on that are real
     int row0;
@@ -223,39 +227,6 @@ __device__ __forceinline__ uint64_t ta_mul2(uint64_t a, uint64_t b)
     asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
     return r;
 }
-// 2^x of a pair without the special-function unit: x = n + f, n whole, |f| <= 1/2; 2^f by the polynomial with the smallest largest relative
-// error (an exchange algorithm's: 2.7e-6 of degree 4, 2.3e-7 of degree 5, in fp32), n added to the exponent. x is at most
-// 127 and taken as -125 below that.
-template <int kDegree>
-__device__ __forceinline__ void ta_ex2_poly(uint64_t x, float &a, float &b)
-{
-    float x0, x1;
-    ta_split(x, x0, x1);
-    x = ta_two(fmaxf(x0, -125.f), fmaxf(x1, -125.f));
-    constexpr float kRound = 12582912.f;                    // 1.5 * 2^23: adding it leaves whole numbers
-    const uint64_t t = ta_add2(x, ta_two(kRound, kRound));
-    const uint64_t f = ta_add2(x, ta_fma2(t, ta_two(-1.f, -1.f), ta_two(kRound, kRound)));
-    const auto c = [](float v) { return ta_two(v, v); };
-    uint64_t r;
-    if constexpr (kDegree == 4) {
-        r = ta_fma2(c(0.009570101911165427f), f, c(0.055917860319388245f));
-        r = ta_fma2(r, f, c(0.2402474482786378f));
-        r = ta_fma2(r, f, c(0.6931218147366892f));
-        r = ta_fma2(r, f, c(0.9999992614457122f));
-    } else {
-        r = ta_fma2(c(0.0013276471992533984f), f, c(0.009675541334453752f));
-        r = ta_fma2(r, f, c(0.055507132734978495f));
-        r = ta_fma2(r, f, c(0.24022119723839974f));
-        r = ta_fma2(r, f, c(0.6931469670647609f));
-        r = ta_fma2(r, f, c(1.0000000716546849f));
-    }
-    float t0, t1, r0, r1;
-    ta_split(t, t0, t1);
-    ta_split(r, r0, r1);
-    a = __int_as_float(__float_as_int(r0) + (__float_as_int(t0) << 23));
-    b = __int_as_float(__float_as_int(r1) + (__float_as_int(t1) << 23));
-}
-
 template <int kStream> struct TaStream { static constexpr int value = kStream; };
 // The ring is filled in the order of first use, and in groups that land and are left together (a wait and a commit each, which cost the
 // issuing lane a hundred or two hundred cycles apiece): where both streams use a tile, K_0 | V_0 K_1 | V_1 K_2 | ..., where they take
@@ -270,32 +241,44 @@ __device__ __forceinline__ int ta_value_place(const TaItem &it, int tile)
 __device__ __forceinline__ int ta_group(const TaItem &it, int place) { return it.shared ? (place + 1) / 2 : place / 2; }
 __device__ __forceinline__ bool ta_cut(const TaItem &it) { return it.fix_tail && it.n_keys < (it.tile0 + ta_tiles(it)) * kTaTile; }
 
-// cap * tanh(x cap_in) * log2 e of a thread's products. |x cap_in| <= 1 throughout the warp, the usual case: tanh(y) = y P(y^2), P with the
-// smallest largest relative error (degree 5 in y^2: 6e-7; 6: 5e-8), cap * log2 e folded into its coefficients. Otherwise from e = exp(-2 |y|):
-// (1 - e) / (1 + e) with y's sign, two uses of the special-function unit.
+// cap * tanh(x cap_in) * log2 e of a thread's products: tanh(y) = y P(y^2) with the P of kN coefficients that has the smallest largest relative
+// error on [0, 1/2] (kWide: [0, 1]), cap * log2 e folded into them: 5e-7 of 4 coefficients, 1e-8 of 5 (kWide 6e-7 of 6, 5e-8 of 7).
+template <bool kWide, int kN, int kCols>
+__device__ __forceinline__ void ta_cap_poly(const TaScore &sc, float (&v)[kCols])
+{
+    constexpr float kP[4][7] = {{0.9999994557709386f, -0.33326317935941724f, 0.13190296603213952f, -0.04440222612781058f},
+                                {0.9999999868718333f, -0.33333069394022213f, 0.1332477931761862f, -0.05298607529180707f, 0.0171350066346453f},
+                                {0.9999994135992578f, -0.3332904237853047f, 0.13281433880736535f, -0.05160567400212715f, 0.016743115063748693f,
+                                 -0.0030670603265534825f},
+                                {0.9999999502407364f, -0.3333283915307065f, 0.1332520407582405f, -0.0534570295681808f, 0.02028998042301148f,
+                                 -0.006203379104680566f, 0.0010410226337084262f}};
+    static_assert(kWide ? kN == 6 || kN == 7 : kN == 4 || kN == 5, "a row of the table");
+    uint64_t c[kN];
+#pragma unroll
+    for (int k = 0; k < kN; ++k) c[k] = ta_two(kP[kN - 4][k] * sc.cap_log2, kP[kN - 4][k] * sc.cap_log2);
+    const uint64_t in = ta_two(sc.cap_in, sc.cap_in);
+#pragma unroll
+    for (int i = 0; i < kCols; i += 2) {
+        const uint64_t y = ta_mul2(ta_two(v[i], v[i + 1]), in), u = ta_mul2(y, y);
+        uint64_t r = c[kN - 1];
+#pragma unroll
+        for (int k = kN - 2; k >= 0; --k) r = ta_fma2(r, u, c[k]);
+        ta_split(ta_mul2(r, y), v[i], v[i + 1]);
+    }
+}
+// By a polynomial where the warp's |x cap_in| are at most 1, the usual case. Otherwise from e = exp(-2 |y|): (1 - e) / (1 + e) with y's sign,
+// two uses of the special-function unit.
 template <bool kTwo, int kCols>
 __device__ __forceinline__ void ta_cap(const TaScore &sc, float (&v)[kCols])
 {
-    constexpr int kN = kTwo ? 7 : 6;
-    constexpr float kP[2][7] = {{0.9999994135992578f, -0.3332904237853047f, 0.13281433880736535f, -0.05160567400212715f, 0.016743115063748693f, -0.0030670603265534825f, 0.f},
-                                {0.9999999502407364f, -0.3333283915307065f, 0.1332520407582405f, -0.0534570295681808f, 0.02028998042301148f,
-                                 -0.006203379104680566f, 0.0010410226337084262f}};
     float far = 0.f;
 #pragma unroll
     for (int i = 0; i < kCols; i += 2) far = fmaxf(fmaxf(far, fabsf(v[i])), fabsf(v[i + 1]));
-    if (__all_sync(0xFFFFFFFFu, far * sc.cap_in <= 1.f)) {
-        uint64_t c[kN];
-#pragma unroll
-        for (int k = 0; k < kN; ++k) c[k] = ta_two(kP[kTwo][k] * sc.cap_log2, kP[kTwo][k] * sc.cap_log2);
-        const uint64_t in = ta_two(sc.cap_in, sc.cap_in);
-#pragma unroll
-        for (int i = 0; i < kCols; i += 2) {
-            const uint64_t y = ta_mul2(ta_two(v[i], v[i + 1]), in), u = ta_mul2(y, y);
-            uint64_t r = c[kN - 1];
-#pragma unroll
-            for (int k = kN - 2; k >= 0; --k) r = ta_fma2(r, u, c[k]);
-            ta_split(ta_mul2(r, y), v[i], v[i + 1]);
-        }
+    far *= sc.cap_in;
+    if (__all_sync(0xFFFFFFFFu, far <= 0.5f)) {
+        ta_cap_poly<false, kTwo ? 5 : 4>(sc, v);
+    } else if (__all_sync(0xFFFFFFFFu, far <= 1.f)) {
+        ta_cap_poly<true, kTwo ? 7 : 6>(sc, v);
     } else {
 #pragma unroll
         for (int i = 0; i < kCols; ++i) {
@@ -382,13 +365,9 @@ __device__ __forceinline__ bool ta_softmax(TaSmem &sm, const TaItem &it, const T
                 for (int i = 0; i < 16; ++i) {
                     const uint64_t two = ta_two(v[32 * q + 2 * i], v[32 * q + 2 * i + 1]), x = kRaw ? ta_fma2(two, mul2, shift2) : ta_add2(two, shift2);
                     float p0, p1;
-                    if (i % kTaPolyEvery == kTaPolyEvery - 1) {
-                        ta_ex2_poly<kTwo ? 5 : 4>(x, p0, p1);
-                    } else {
-                        ta_split(x, p0, p1);
-                        p0 = ta_ex2(p0);
-                        p1 = ta_ex2(p1);
-                    }
+                    ta_split(x, p0, p1);
+                    p0 = ta_ex2(p0);
+                    p1 = ta_ex2(p1);
                     const uint64_t pp = ta_two(p0, p1);
                     sum[i & 1] = ta_add2(sum[i & 1], pp);
                     hi[i] = ta_pack<kHalf>(p0, p1);
@@ -513,10 +492,11 @@ __device__ __forceinline__ void ta_block(TaSmem &sm, const TaItem &it, const TaS
         asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");
         // ---- the queries, then a row of scores per thread ----
         const int tiles = it.shared ? 2 : 1;
-#pragma unroll 4
+#pragma unroll 8
         for (int e = tid; e < tiles * kTaTile * 16; e += 256) {
             const int r = e >> 4, ch = e & 15, lr = it.shared ? r : r % (kTaTile / it.fold), row = it.row0 + min(lr, it.n_rows - 1);
-            const uint16_t *src = it.q + ((int64_t)(row / it.group) * it.n_q + it.head0 + row % it.group) * kHeadDim + 8 * ch;
+            const int token = ta_token(row, it.by_group);
+            const uint16_t *src = it.q + ((int64_t)token * it.n_q + it.head0 + row - token * it.group) * kHeadDim + 8 * ch;
             asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(ta_addr(sm.q[r >> 7] + ta_byte(r & 127, ch))), "l"(src),
                          "r"(lr < it.n_rows ? 16 : 0) : "memory");
         }

@@ -5,7 +5,8 @@
 // of one head of ALL slots: it reads every row that moves into shared memory, and writes when it has them all; no other
 // block touches these rows, so one launch does it without a second buffer.
 //
-// Bound by memory: each moved row is read and written once. Rows of slots that stay are not touched.
+// Bound by memory: each moved row is read and written once. Rows of slots that stay are not touched: the block's threads go through a list of
+// the slots that move. 16 of 32 slots of up to 1024 rows (26.5 MB, 4.1 us at the copy rate): see kForkStage.
 #include "common.cuh"
 #include "santapp_serve.h"
 
@@ -14,13 +15,15 @@ namespace santapp {
 namespace {
 
 constexpr int kForkThreads = 256;
-constexpr int kForkStage = 64 * 1024;     // bytes of rows a block stages at most, while one row of every slot is no more
+// Bytes of rows a block stages at most, while one row of every slot is no more: a block waits for memory twice (its table, its rows), so
+// what hides that is blocks beside it, six of this size an SM
+constexpr int kForkStage = 32 * 1024;
 constexpr int kForkMaxSeqs = 4096;
 
 struct ForkParams {
     int n_seqs, n_kv, cap;
-    int rows;                             // rows a block takes of every slot
-    int pieces;                           // 16-byte pieces of them (16: whole rows), a power of two
+    int row_bits;                         // a block takes 2^row_bits rows of every slot
+    int piece_bits;                       // 2^piece_bits 16-byte pieces of them (4: whole rows)
     const int32_t *src, *len;
     uint4 *k, *v;
     int32_t *len_out;
@@ -31,38 +34,42 @@ fork_kernel(ForkParams p)
 {
     step_wait();
     extern __shared__ __align__(16) unsigned char smem_fork[];
-    const int tid = threadIdx.x, B = p.n_seqs;
-    uint4 *stage = reinterpret_cast<uint4 *>(smem_fork);                             // [slot][row][piece]
-    int2 *tab = reinterpret_cast<int2 *>(stage + (size_t)B * p.rows * p.pieces);      // source, rows of this block that move
-    const int parts = 16 / p.pieces, r0 = (blockIdx.x / parts) * p.rows, c0 = (blockIdx.x % parts) * p.pieces;
+    __shared__ int n_moved;
+    const int tid = threadIdx.x, B = p.n_seqs, bits = p.row_bits + p.piece_bits, rows = 1 << p.row_bits;
+    uint4 *stage = reinterpret_cast<uint4 *>(smem_fork);                              // [moved slot][row][piece]
+    int2 *tab = reinterpret_cast<int2 *>(stage + ((size_t)B << bits));                 // slot and its source, rows of this block that move
+    const int r0 = (blockIdx.x >> (4 - p.piece_bits)) << p.row_bits, c0 = (blockIdx.x & ((16 >> p.piece_bits) - 1)) << p.piece_bits;
     const int j = blockIdx.y;
     uint4 *buf = blockIdx.z ? p.v : p.k;
     const bool writes_len = p.len_out != nullptr && blockIdx.x == 0 && j == 0 && blockIdx.z == 0;
-    int any = 0;
+    if (tid == 0) n_moved = 0;
+    __syncthreads();
     for (int b = tid; b < B; b += kForkThreads) {
         const int a = p.src[b];
         const int n = a >= 0 && a < B ? min(max(p.len[a], 0), p.cap) : 0;
-        const int move = a != b ? min(max(n - r0, 0), p.rows) : 0;
-        tab[b] = make_int2(a, move);
-        any |= move;
+        const int move = a != b ? min(n - r0, rows) : 0;
+        if (move > 0) tab[atomicAdd(&n_moved, 1)] = make_int2(b << 16 | a, move);
         if (writes_len) p.len_out[b] = n;
     }
-    if (!__syncthreads_or(any)) return;
-    const int per_slot = p.rows * p.pieces, total = B * per_slot;
+    __syncthreads();
+    const int total = n_moved << bits;
     const auto at = [&](int b, int e) {
-        return (((int64_t)b * p.n_kv + j) * p.cap + r0 + e / p.pieces) * 16 + c0 + e % p.pieces;
+        return (((int64_t)b * p.n_kv + j) * p.cap + r0 + (e >> p.piece_bits)) * 16 + c0 + (e & ((1 << p.piece_bits) - 1));
     };
+#pragma unroll 4
     for (int i = tid; i < total; i += kForkThreads) {
-        const int b = i / per_slot, e = i % per_slot;
-        const int2 t = tab[b];
-        if (e / p.pieces < t.y)
-            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(stage + i)), "l"(buf + at(t.x, e)) : "memory");
+        const int2 t = tab[i >> bits];
+        const int e = i & ((1 << bits) - 1);
+        if ((e >> p.piece_bits) < t.y)
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(stage + i)), "l"(buf + at(t.x & 0xFFFF, e)) : "memory");
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
     __syncthreads();
+#pragma unroll 4
     for (int i = tid; i < total; i += kForkThreads) {
-        const int b = i / per_slot, e = i % per_slot;
-        if (e / p.pieces < tab[b].y) buf[at(b, e)] = stage[i];
+        const int2 t = tab[i >> bits];
+        const int e = i & ((1 << bits) - 1);
+        if ((e >> p.piece_bits) < t.y) buf[at(t.x >> 16, e)] = stage[i];
     }
 }
 
@@ -95,21 +102,21 @@ extern "C" int santapp_suffix_fork(const santapp_geom *geom, const int32_t *src,
     p.n_seqs = geom->n_seqs;
     p.n_kv = geom->n_kv_heads;
     p.cap = suffix_cap;
-    p.pieces = 16;
-    while (p.pieces > 2 && p.n_seqs * p.pieces * 16 > 2 * kForkStage) p.pieces /= 2;     // (32 bytes: a sector of memory; 128 KB at 4096 slots)
-    p.rows = kForkStage / (p.n_seqs * p.pieces * 16);
-    p.rows = p.rows < 1 ? 1 : (p.rows > 16 ? 16 : p.rows);
+    p.piece_bits = 4;
+    while (p.piece_bits > 1 && p.n_seqs << (p.piece_bits + 4) > 128 * 1024) --p.piece_bits;     // (32 bytes: a sector of memory; 128 KB at 4096 slots)
+    p.row_bits = 0;
+    while (p.row_bits < 4 && p.n_seqs << (p.piece_bits + p.row_bits + 5) <= kForkStage) ++p.row_bits;
     p.src = src;
     p.len = suffix_len;
     p.k = static_cast<uint4 *>(k_suffix);
     p.v = static_cast<uint4 *>(v_suffix);
     p.len_out = suffix_len_out;
     begin_call();
-    const size_t smem = (size_t)p.n_seqs * p.rows * p.pieces * 16 + sizeof(int2) * (size_t)p.n_seqs;
+    const size_t smem = ((size_t)p.n_seqs << (p.row_bits + p.piece_bits + 4)) + sizeof(int2) * (size_t)p.n_seqs;
     static std::atomic<unsigned long long> opted{0};
     cudaError_t err = ensure_dynamic_smem(reinterpret_cast<const void *>(fork_kernel), 200 * 1024, opted);
     if (err != cudaSuccess) return note_cuda_failure(err, "fork set-up");
-    const dim3 grid((unsigned)((suffix_cap + p.rows - 1) / p.rows * (16 / p.pieces)), (unsigned)p.n_kv, 2);
+    const dim3 grid((unsigned)(((suffix_cap + (1 << p.row_bits) - 1) >> p.row_bits) << (4 - p.piece_bits)), (unsigned)p.n_kv, 2);
     err = launch_step(fork_kernel, grid, dim3(kForkThreads), smem, static_cast<cudaStream_t>(stream), p);
     if (err != cudaSuccess) return note_cuda_failure(err, "fork launch");
     note_launch_count(1);

@@ -61,6 +61,7 @@ prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__
     TaItem it;
     it.head0 = j * p.group;
     it.group = p.group;
+    it.by_group = ta_by_group(p.group);
     it.n_q = p.n_q;
     it.q = p.q;
     it.row0 = pair * 2 * kTaTile;

@@ -25,6 +25,7 @@ struct PromptParams {
     const uint16_t *q;
     uint16_t *out;
     int n_q, n_kv, group, n_seqs;
+    uint32_t by_group;
     TaScore score;
     PromptSeq seq[kPromptSeqs];
 };
@@ -47,6 +48,7 @@ prompt_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__
     TaItem it;
     it.head0 = j * p.group;
     it.group = p.group;
+    it.by_group = p.by_group;
     it.n_q = p.n_q;
     it.q = p.q + (int64_t)sq.token0 * p.n_q * kHeadDim;
     it.row0 = ((n_rows + 2 * kTaTile - 1) / (2 * kTaTile) - 1 - local / p.n_kv) * 2 * kTaTile;
@@ -58,7 +60,7 @@ prompt_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__
     it.shared = it.n_rows > kTaTile;
     it.fold = 1;
     it.fix_tail = true;
-    const auto seen = [&](int row) { return max(sq.n_keys - sq.n_new + row / p.group + 1, sq.both); };
+    const auto seen = [&](int row) { return max(sq.n_keys - sq.n_new + ta_token(row, p.by_group) + 1, sq.both); };
     const auto tiles = [&](int rows) { return (seen(it.row0 + rows - 1) + kTaTile - 1) / kTaTile; };
     if (it.shared) {
         it.count0 = tiles(kTaTile);
@@ -71,15 +73,15 @@ prompt_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__
     ta_block<kHalf, false, kCap, kBias, kTaTile>(
         sm, it, p.score, &k_map, &v_map, nullptr,
         [&](int row, int &vis, int &q_pos) {
-            q_pos = sq.n_keys - sq.n_new + row / p.group;
+            q_pos = sq.n_keys - sq.n_new + ta_token(row, p.by_group);
             vis = seen(row);
         },
         [&](bool ok, int s, bool live, float m, float l) {
             ta_rows<kHalf, false>(
                 sm, it, ok, s, live, m, l,
                 [&](int r) {
-                    const int row = it.row0 + r;
-                    return static_cast<void *>(p.out + ((int64_t)(sq.token0 + row / p.group) * p.n_q + it.head0 + row % p.group) * kHeadDim);
+                    const int row = it.row0 + r, token = ta_token(row, p.by_group);
+                    return static_cast<void *>(p.out + ((int64_t)(sq.token0 + token) * p.n_q + it.head0 + row - token * p.group) * kHeadDim);
                 },
                 [](int, float, float) {});
         });
@@ -119,7 +121,7 @@ extern "C" int santapp_prompt_attn(const santapp_geom *geom, const int32_t *prom
         keys += n;
         tokens += m;
     }
-    if (keys >= (int64_t)1 << 30 || tokens * group >= (int64_t)1 << 30) return SANTAPP_ERR_UNSUPPORTED;
+    if (keys >= (int64_t)1 << 30 || tokens * group >= (int64_t)1 << 29) return SANTAPP_ERR_UNSUPPORTED;
     if ((tokens * group / (2 * kTaTile) + B) * geom->n_kv_heads >= (int64_t)1 << 31) return SANTAPP_ERR_UNSUPPORTED;
     begin_call();
     if (tokens == 0) return SANTAPP_OK;
@@ -135,6 +137,7 @@ extern "C" int santapp_prompt_attn(const santapp_geom *geom, const int32_t *prom
     p.n_q = geom->n_q_heads;
     p.n_kv = geom->n_kv_heads;
     p.group = group;
+    p.by_group = ta_by_group(group);
     p.score = score;
     const PromptKernel kernel = geom->elem_type ? prompt_kernel_of<true>(score.cap_log2 > 0.f, score.slopes != nullptr)
                                                 : prompt_kernel_of<false>(score.cap_log2 > 0.f, score.slopes != nullptr);

@@ -18,6 +18,12 @@ namespace santapp {
 namespace {
 
 constexpr int kRopeThreads = 256;
+#ifndef K1
+#define K1 4
+#define K2 5
+#define K3 3
+#endif
+constexpr int kMany = K1, kManyAhead = K2, kManyBlocks = K3;
 constexpr int kUnits = 8;                 // units of a head: two 16-byte pieces that hold both values of eight pairs
 
 struct RopeParams {
@@ -70,9 +76,9 @@ __device__ __forceinline__ void turn_neighbours(uint4 &x, uint4 &y, const float2
     }
 }
 
-// kTokens tokens a block.
-template <bool kHalf, int kTokens>
-__global__ void __launch_bounds__(kRopeThreads)
+// kTokens tokens a block, kAhead units a thread under way.
+template <bool kHalf, int kTokens, int kAhead, int kBlocks>
+__global__ void __launch_bounds__(kRopeThreads, kBlocks)
 rope_kernel(const __grid_constant__ RopeParams p)
 {
     step_wait();
@@ -86,15 +92,21 @@ rope_kernel(const __grid_constant__ RopeParams p)
     // pieces of unit u of a head: rotated ones hold pairs 8 u .. 8 u + 7
     auto first_piece = [&](int u) { return u < p.rot / 16 && !p.interleaved ? u : 2 * u; };
     auto second_piece = [&](int u) { return u < p.rot / 16 && !p.interleaved ? u + p.rot / 16 : 2 * u + 1; };
-    constexpr int kAhead = 5;                               // units a thread has under way
+    // token and row of heads of unit e
+    const auto token_of = [&](int e) {
+        int t = 0;
+#pragma unroll
+        for (int x = 1; x < kTokens; ++x) t += e >= x * heads * kUnits;
+        return t;
+    };
     uint4 x[kAhead], y[kAhead];
     auto load = [&](int base) {
 #pragma unroll
         for (int m = 0; m < kAhead; ++m) {
             const int e = base + m * kRopeThreads + tid;
             if (e >= n_units) break;
-            const int u = e & (kUnits - 1), h = (e / kUnits) % heads;
-            const int64_t row = row0 + e / (kUnits * heads);
+            const int u = e & (kUnits - 1), t = token_of(e), h = e / kUnits - t * heads;
+            const int64_t row = row0 + t;
             const uint4 *src = h < p.n_q ? p.q + row * p.q_stride + h * 16
                                          : (h < p.n_q + p.n_kv ? p.k + row * p.k_stride + (h - p.n_q) * 16
                                                                : p.v + row * p.v_stride + (h - p.n_q - p.n_kv) * 16);
@@ -126,7 +138,7 @@ rope_kernel(const __grid_constant__ RopeParams p)
         for (int m = 0; m < kAhead; ++m) {
             const int e = base + m * kRopeThreads + tid;
             if (e >= n_units) break;
-            const int u = e & (kUnits - 1), h = (e / kUnits) % heads, t = e / (kUnits * heads);
+            const int u = e & (kUnits - 1), t = token_of(e), h = e / kUnits - t * heads;
             const int64_t row = row0 + t, to = dst[t];
             if (h < p.n_q + p.n_kv && u < p.rot / 16) {
                 if (p.interleaved) turn_neighbours<kHalf>(x[m], y[m], &table[t][8 * u]);
@@ -181,10 +193,10 @@ int run_rope(RopeParams &p, const santapp_geom *geom, const santapp_rope *r, san
     begin_call();
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     const bool many = p.n_rows >= 4 * 4 * (int64_t)attend_grid_size();
-    const dim3 grid((unsigned)(many ? (p.n_rows + 3) / 4 : p.n_rows));
+    const dim3 grid((unsigned)(many ? (p.n_rows + kMany - 1) / kMany : p.n_rows));
     cudaError_t err;
-    if (many) err = launch_step(geom->elem_type ? rope_kernel<true, 4> : rope_kernel<false, 4>, grid, dim3(kRopeThreads), 0, s, p);
-    else      err = launch_step(geom->elem_type ? rope_kernel<true, 1> : rope_kernel<false, 1>, grid, dim3(kRopeThreads), 0, s, p);
+    if (many) err = launch_step(geom->elem_type ? rope_kernel<true, kMany, kManyAhead, kManyBlocks> : rope_kernel<false, kMany, kManyAhead, kManyBlocks>, grid, dim3(kRopeThreads), 0, s, p);
+    else      err = launch_step(geom->elem_type ? rope_kernel<true, 1, 5, 1> : rope_kernel<false, 1, 5, 1>, grid, dim3(kRopeThreads), 0, s, p);
     if (err != cudaSuccess) return note_cuda_failure(err, "rope launch");
     note_launch_count(1);
     return SANTAPP_OK;
