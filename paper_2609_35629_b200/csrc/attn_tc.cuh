@@ -16,9 +16,11 @@
 //
 // Weights: kTwo splits a weight into two 16-bit terms, p = hi + lo (off by at most 2^-16 of it, bf16), two products with V:
 // outputs good to fp32. Without, a weight is rounded once (2^-8, bf16), for outputs that are 16 bits wide anyway.
-// The running maximum is renewed only when a score passes it by 2^kSlack: until then weights are at most 2^kSlack, and O need
-// not be scaled; statistics and sums are fp32. fp16 weights carry a factor 2^7 (at most 2^15; the smallest kept is 2^-31 of one), which
-// cancels in O / l.
+// The running maximum is renewed only when a score passes it by 2^slack: until then weights are at most that, and O need not be scaled, which
+// takes a warp 1200 cycles and is due as soon as one of its 32 rows asks for it (with 2^8, in every second tile of rows whose best key stands
+// out by e^9). Sums, O and bf16 weights have the range of fp32: 2^24 (values of V to 2^80 stay finite). fp16 weights end at 2^16:
+// they carry a factor 2^shift, which cancels in O / l, and slack + shift = 15: 11 + 4, or 8 + 7 for the two terms, whose second
+// loses nothing above 2^-31 of the reference. Statistics and sums are fp32.
 //
 // Every wait is bounded: one that runs out makes all roles of the block stop, waits for its own copies and products, and the
 // results are NaN (and bit 2 of the status word).
@@ -37,7 +39,8 @@ constexpr int kTaThreads = 384;           // warps 0-3, 4-7: a row per thread of
 constexpr int kTaTile = 128;              // query rows of a stream, keys of a tile
 constexpr int kTaTileBytes = kTaTile * kHeadDim * 2;
 constexpr int kTaRing = 5;                // tiles of keys or values under way
-constexpr float kTaSlack = 8.f;
+template <bool kHalf, bool kTwo> constexpr float kTaSlack = !kHalf ? 24.f : (kTwo ? 8.f : 11.f);
+template <bool kHalf, bool kTwo> constexpr float kTaShift = !kHalf ? 0.f : (kTwo ? 7.f : 4.f);
 
 struct TaSmem {
     alignas(1024) unsigned char q[2][kTaTileBytes];
@@ -293,13 +296,13 @@ __device__ __forceinline__ void ta_cap(const TaScore &sc, float (&v)[kCols])
 //
 // What a tile takes between its scores and its weights decides the pace (the products of the other stream are shorter), so the first quarter of the
 // exponentials is taken against the maximum of the tiles before, beside the search for this tile's; where a score passes it by
-// more than 2^kTaSlack, and in the first tile, that quarter is taken again. The last quarter of the weights is handed over on its own: only
+// more than the slack, and in the first tile, that quarter is taken again. The last quarter of the weights is handed over on its own: only
 // its product remains to be done when the last weight is there.
 template <bool kHalf, bool kTwo, bool kCap, bool kBias, int kCols>
 __device__ __forceinline__ bool ta_softmax(TaSmem &sm, const TaItem &it, const TaScore &sc, int s, bool live, int vis, int q_pos,
                                            float slope_log2, const int32_t *key_pos, float &m, float &l)
 {
-    constexpr float kShift = kHalf ? 7.f : 0.f;
+    constexpr float kShift = kTaShift<kHalf, kTwo>;
     constexpr bool kRaw = !kCap && !kBias;                  // scores stay in units of the product, not yet scaled
     const int t = threadIdx.x & 127;
     const uint32_t lanes = (uint32_t)((threadIdx.x >> 5) & 3) << 21;
@@ -391,7 +394,7 @@ __device__ __forceinline__ bool ta_softmax(TaSmem &sm, const TaItem &it, const T
 #pragma unroll
                 for (int x = 0; x < 4; ++x) top[x] = i + 4 + x < kCols ? fmaxf(fmaxf(top[x], v[i + x]), v[i + 4 + x]) : fmaxf(top[x], v[i + x]);
             const float m_new = fmaxf(m, mul * fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])));
-            if (__any_sync(0xFFFFFFFFu, m_new > m + (c == 0 ? 0.f : kTaSlack))) {
+            if (__any_sync(0xFFFFFFFFu, m_new > m + (c == 0 ? 0.f : kTaSlack<kHalf, kTwo>))) {
                 if (c > 0) {
                     const float f = m_new == -CUDART_INF_F ? 1.f : ta_ex2(m - m_new);
                     float o[16];
