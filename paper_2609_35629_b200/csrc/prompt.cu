@@ -2,7 +2,8 @@
 //
 // A block takes 256 query rows (a KV head's query heads of 256 / group tokens) of one sequence and every key tile that one of them sees:
 // 4 d operations per query head and visible pair, far more than the bytes, so tensor cores and exponentials bound
-// it. Blocks run from the longest sequence's last rows (which see most keys) down, so that the last ones are short.
+// it. Blocks run from the longest sequence's last rows (which see most keys) down, so that the last ones are short. Where 256 rows a
+// block leave SMs idle or the longest block alone (item_rows), a block takes 128, whose two streams share the keys.
 // The sequences' tables travel in the kernel's arguments, kPromptSeqs at a launch.
 #include <algorithm>
 #include <math.h>
@@ -24,7 +25,7 @@ struct PromptSeq {
 struct PromptParams {
     const uint16_t *q;
     uint16_t *out;
-    int n_q, n_kv, group, n_seqs;
+    int n_q, n_kv, group, n_seqs, item_rows;
     uint32_t by_group;
     TaScore score;
     PromptSeq seq[kPromptSeqs];
@@ -51,8 +52,8 @@ prompt_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__
     it.by_group = p.by_group;
     it.n_q = p.n_q;
     it.q = p.q + (int64_t)sq.token0 * p.n_q * kHeadDim;
-    it.row0 = ((n_rows + 2 * kTaTile - 1) / (2 * kTaTile) - 1 - local / p.n_kv) * 2 * kTaTile;
-    it.n_rows = min(2 * kTaTile, n_rows - it.row0);
+    it.row0 = ((n_rows + p.item_rows - 1) / p.item_rows - 1 - local / p.n_kv) * p.item_rows;
+    it.n_rows = min(p.item_rows, n_rows - it.row0);
     it.plane = j;
     it.key0 = sq.key0;
     it.n_keys = sq.n_keys;
@@ -85,6 +86,28 @@ prompt_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__
                 },
                 [](int, float, float) {});
         });
+}
+
+// Query rows a block takes: what ends first when blocks are dealt out from the longest down. A tile of keys costs a block of 256 rows a
+// step, one of 128 half a step (its streams take tiles in turn), either kOverhead steps to begin and end.
+int item_rows(const PromptSeq *seq, int n, int group, int n_kv)
+{
+    constexpr double kOverhead = 4.0;
+    double best = 1e300;
+    int rows = 2 * kTaTile;
+    for (int size = 2 * kTaTile; size >= kTaTile; size /= 2) {
+        const double step = size == kTaTile ? 0.5 : 1.0;
+        double total = 0.0, longest = 0.0;
+        for (int i = 0; i < n; ++i) {
+            const double items = (double)(((int64_t)seq[i].n_new * group + size - 1) / size);
+            const double last = std::max((double)seq[i].n_keys, (double)seq[i].both) / kTaTile, first = std::max(last - (double)seq[i].n_new / kTaTile, (double)seq[i].both / kTaTile);
+            total += items * n_kv * (step * 0.5 * (first + last + 1.0) + kOverhead);
+            longest = std::max(longest, step * (last + 0.5) + kOverhead);
+        }
+        const double cost = std::max(longest, total / attend_grid_size() + 0.5 * longest);
+        if (cost < best) best = cost, rows = size;
+    }
+    return rows;
 }
 
 bool misaligned(const void *p, size_t a) { return p != nullptr && (reinterpret_cast<uintptr_t>(p) % a) != 0; }
@@ -122,7 +145,7 @@ extern "C" int santapp_prompt_attn(const santapp_geom *geom, const int32_t *prom
         tokens += m;
     }
     if (keys >= (int64_t)1 << 30 || tokens * group >= (int64_t)1 << 29) return SANTAPP_ERR_UNSUPPORTED;
-    if ((tokens * group / (2 * kTaTile) + B) * geom->n_kv_heads >= (int64_t)1 << 31) return SANTAPP_ERR_UNSUPPORTED;
+    if ((tokens * group / kTaTile + B) * geom->n_kv_heads >= (int64_t)1 << 31) return SANTAPP_ERR_UNSUPPORTED;
     begin_call();
     if (tokens == 0) return SANTAPP_OK;
     CUtensorMap k_map, v_map;
@@ -158,9 +181,10 @@ extern "C" int santapp_prompt_attn(const santapp_geom *geom, const int32_t *prom
         if (n == 0) continue;
         std::sort(p.seq, p.seq + n, [](const PromptSeq &x, const PromptSeq &y) { return x.n_keys != y.n_keys ? x.n_keys > y.n_keys : x.key0 < y.key0; });
         int items = 0;
+        p.item_rows = item_rows(p.seq, n, group, geom->n_kv_heads);
         for (int i = 0; i < n; ++i) {
             p.seq[i].item0 = items;
-            items += (p.seq[i].n_new * group + 2 * kTaTile - 1) / (2 * kTaTile) * geom->n_kv_heads;
+            items += (p.seq[i].n_new * group + p.item_rows - 1) / p.item_rows * geom->n_kv_heads;
         }
         p.n_seqs = n;
         err = launch_step(kernel, dim3((unsigned)items), dim3(kTaThreads), kTaSmemBytes, static_cast<cudaStream_t>(stream), k_map, v_map, p);
