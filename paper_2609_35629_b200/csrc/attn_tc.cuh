@@ -261,12 +261,20 @@ __device__ __forceinline__ void ta_cap_poly(const TaScore &sc, float (&v)[kCols]
     for (int k = 0; k < kN; ++k) c[k] = ta_two(kP[kN - 4][k] * sc.cap_log2, kP[kN - 4][k] * sc.cap_log2);
     const uint64_t in = ta_two(sc.cap_in, sc.cap_in);
 #pragma unroll
-    for (int i = 0; i < kCols; i += 2) {
-        const uint64_t y = ta_mul2(ta_two(v[i], v[i + 1]), in), u = ta_mul2(y, y);
-        uint64_t r = c[kN - 1];
+    for (int i = 0; i < kCols; i += 8) {                    // four pairs side by side: one alone waits for each of its products
+        uint64_t y[4], u[4], r[4];
 #pragma unroll
-        for (int k = kN - 2; k >= 0; --k) r = ta_fma2(r, u, c[k]);
-        ta_split(ta_mul2(r, y), v[i], v[i + 1]);
+        for (int x = 0; x < 4; ++x) y[x] = ta_mul2(ta_two(v[i + 2 * x], v[i + 2 * x + 1]), in);
+#pragma unroll
+        for (int x = 0; x < 4; ++x) u[x] = ta_mul2(y[x], y[x]);
+#pragma unroll
+        for (int x = 0; x < 4; ++x) r[x] = ta_fma2(c[kN - 1], u[x], c[kN - 2]);
+#pragma unroll
+        for (int k = kN - 3; k >= 0; --k)
+#pragma unroll
+            for (int x = 0; x < 4; ++x) r[x] = ta_fma2(r[x], u[x], c[k]);
+#pragma unroll
+        for (int x = 0; x < 4; ++x) ta_split(ta_mul2(r[x], y[x]), v[i + 2 * x], v[i + 2 * x + 1]);
     }
 }
 // By a polynomial where the warp's |x cap_in| are at most 1, the usual case. Otherwise from e = exp(-2 |y|): (1 - e) / (1 + e) with y's sign,
@@ -274,10 +282,12 @@ __device__ __forceinline__ void ta_cap_poly(const TaScore &sc, float (&v)[kCols]
 template <bool kTwo, int kCols>
 __device__ __forceinline__ void ta_cap(const TaScore &sc, float (&v)[kCols])
 {
-    float far = 0.f;
+    float most[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int i = 0; i < kCols; i += 2) far = fmaxf(fmaxf(far, fabsf(v[i])), fabsf(v[i + 1]));
-    far *= sc.cap_in;
+    for (int i = 0; i < kCols; i += 8)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) most[x] = fmaxf(fmaxf(most[x], fabsf(v[i + x])), fabsf(v[i + 4 + x]));
+    const float far = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3])) * sc.cap_in;
     if (__all_sync(0xFFFFFFFFu, far <= 0.5f)) {
         ta_cap_poly<false, kTwo ? 5 : 4>(sc, v);
     } else if (__all_sync(0xFFFFFFFFu, far <= 1.f)) {
