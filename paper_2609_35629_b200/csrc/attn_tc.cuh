@@ -476,7 +476,21 @@ __device__ __forceinline__ void ta_block(TaSmem &sm, const TaItem &it, const TaS
                                          const int32_t *key_pos, Rows rows, Finish finish)
 {
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    if (tid == 0) {
+    if (warp < 8) {                                         // the queries, on their way while the rest is set up
+        const int tiles = it.shared ? 2 : 1;
+#pragma unroll 8
+        for (int e = tid; e < tiles * kTaTile * 16; e += 256) {
+            const int r = e >> 4, ch = e & 15, lr = it.shared ? r : r % (kTaTile / it.fold), row = it.row0 + min(lr, it.n_rows - 1);
+            const int token = ta_token(row, it.by_group);
+            const uint16_t *src = it.q + ((int64_t)token * it.n_q + it.head0 + row - token * it.group) * kHeadDim + 8 * ch;
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(ta_addr(sm.q[r >> 7] + ta_byte(r & 127, ch))), "l"(src),
+                         "r"(lr < it.n_rows ? 16 : 0) : "memory");
+        }
+    } else if (tid == 256) {
+        asm volatile("prefetch.tensormap [%0];" ::"l"(k_map) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(v_map) : "memory");
+    }
+    if (tid == 288) {
         sm.failed = 0;
         for (int i = 0; i < 4; ++i) {
             asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(ta_addr(&sm.full[i])), "r"(2));
@@ -492,7 +506,7 @@ __device__ __forceinline__ void ta_block(TaSmem &sm, const TaItem &it, const TaS
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == 9) {
+    if (warp == 10) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(ta_addr(&sm.tmem)), "r"(512) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::);
     }
@@ -503,16 +517,7 @@ __device__ __forceinline__ void ta_block(TaSmem &sm, const TaItem &it, const TaS
     // registers: 168 a thread at launch; the softmax warps take what the other four leave (8 * 192 + 4 * 120 = 12 * 168)
     if (warp < 8) {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");
-        // ---- the queries, then a row of scores per thread ----
-        const int tiles = it.shared ? 2 : 1;
-#pragma unroll 8
-        for (int e = tid; e < tiles * kTaTile * 16; e += 256) {
-            const int r = e >> 4, ch = e & 15, lr = it.shared ? r : r % (kTaTile / it.fold), row = it.row0 + min(lr, it.n_rows - 1);
-            const int token = ta_token(row, it.by_group);
-            const uint16_t *src = it.q + ((int64_t)token * it.n_q + it.head0 + row - token * it.group) * kHeadDim + 8 * ch;
-            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(ta_addr(sm.q[r >> 7] + ta_byte(r & 127, ch))), "l"(src),
-                         "r"(lr < it.n_rows ? 16 : 0) : "memory");
-        }
+        // ---- a row of scores per thread ----
         asm volatile("cp.async.wait_all;" ::: "memory");
         proxy_fence();
         mbar_arrive(ta_addr(&sm.q_ready));
@@ -652,7 +657,7 @@ __device__ __forceinline__ void ta_block(TaSmem &sm, const TaItem &it, const TaS
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    if (warp == 9) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(sm.tmem), "r"(512));
+    if (warp == 10) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(sm.tmem), "r"(512));
 }
 
 __device__ __forceinline__ void *ta_shfl(void *p, int lane)

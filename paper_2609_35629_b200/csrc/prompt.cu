@@ -8,7 +8,6 @@
 #include <algorithm>
 #include <math.h>
 #include <string.h>
-#include <vector>
 
 #include "attn_tc.cuh"
 #include "santapp_serve.h"
