@@ -637,6 +637,7 @@ __device__ __forceinline__ void ta_block(TaSmem &sm, const TaItem &it, const TaS
                         tc_commit(ta_addr(&sm.left[(t1 + 1) & 3]));
                     }
                 }
+                ok = ok && ta_wait(sm, &sm.left[n_tiles & 3], (uint32_t)(n_tiles >> 2) & 1u);      // (its own last arrival)
                 if (!ok) {                                 // products under way finish before their memory goes
                     for (int i = 0; i < 4096; ++i) __nanosleep(256);
                     if (sc.status != nullptr) atomicOr(sc.status, 4);

@@ -536,10 +536,11 @@ int santapp_prefix_decode_attn(const santapp_geom *geom, const void *k_prefix, c
         if (err != cudaSuccess) return note_cuda_failure(err, "prefix attention launch");
         ++launches;
     }
-    // blocks of a cluster: as many as the SMs hold of all pairs at two each, and as there is work for
+    // blocks of a cluster: no more than there is work for, and all clusters about one block an SM (of eight pairs' worth more, some
+    // clusters find no room beside the others and come second: 12.5 us in place of 8)
     const int pairs = p.n_seqs * p.n_kv, work = std::max((suffix_cap + kFinishBlock - 1) / kFinishBlock, L.parts);
     int blocks = 1;
-    while (blocks < kMaxCluster && 2 * blocks * pairs <= 2 * attend_grid_size() && blocks * kFinishWarps < work) blocks *= 2;
+    while (blocks < kMaxCluster && 2 * blocks * pairs <= attend_grid_size() * 9 / 8 && blocks * kFinishWarps < work) blocks *= 2;
     cudaLaunchAttribute attrs[2];
     attrs[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attrs[0].val.programmaticStreamSerializationAllowed = 1;
