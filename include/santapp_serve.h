@@ -36,7 +36,7 @@ typedef struct santapp_rope {
     int32_t rot_dim;           /* rotated values of a head: a multiple of 16, 16..128               */
     int32_t interleaved;       /* 0: pair i is (i, i + rot_dim / 2); 1: (2 i, 2 i + 1)              */
     double amplitude;          /* 1, or what a long-context scaling multiplies the rotation by      */
-    double inv_freq[64];       /* radians per position of pairs 0 .. rot_dim / 2 - 1                */
+    double inv_freq[64];       /* radians per position of pairs 0 .. rot_dim / 2 - 1 (at most 1e6)  */
 } santapp_rope;
 
 /*
@@ -76,7 +76,7 @@ int santapp_rope_append(const santapp_geom *geom, const santapp_rope *rope, cons
  *   q, k, v, strides  as above, n_rows tokens
  *   positions         device int32 [n_rows], or NULL: position i
  *   dst_row           device int32 [n_rows], or NULL: row i. Rows outside [0, plane_rows) are not
- *                     written; two rows with one destination leave either
+ *                     written; two rows with one destination leave a mixture of the two
  *   q_out             device [n_rows][n_q_heads][d], out (may be q, as above)
  *   k_prompt,v_prompt device [n_kv_heads][plane_rows][d], out: the layout of santapp_build_teams
  * geom->n_seqs is not used.
@@ -121,8 +121,9 @@ typedef struct santapp_attn_opts {
  *                     (plane_rows >= prefix_len): a prompt in token order, or k_packed / v_packed of
  *                     records built for one sequence (attention does not depend on row order)
  *   prefix_len        host; 0: there is no prefix (the two pointers may be NULL)
- *   prefix_token      device int32 planes like the rows' (plane_rows apart): position of each row;
- *                     NULL: row i is at position i. Read only with slopes (row_token of records)
+ *   prefix_token      device int32 planes like the rows' (plane_rows apart): position of each row, in
+ *                     [0, prefix_len); NULL: row i is at position i. Read only with slopes (row_token of
+ *                     records)
  *   q                 device [n_seqs][n_q_heads][d], at position prefix_len + suffix_len[b] - 1
  *   k_suffix, v_suffix, suffix_len_dev, suffix_cap   as in santapp_decode_attn; suffix row i is at
  *                     position prefix_len + i

@@ -6,7 +6,7 @@
 //
 // Bound by memory: every value is read once and written once (18.4 KB each way for a token of 28 + 4 + 4 heads). All heads of
 // a token share its 64 angles: a block computes them once, a pair per thread, into shared memory, behind the loads
-// of its rows, which are all under way before.
+// of its rows, which are under way before.
 #include <math.h>
 #include <string.h>
 

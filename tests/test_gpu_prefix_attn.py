@@ -126,13 +126,45 @@ def test_rows_behind_the_prefix_reach_nothing():
     assert torch.equal(got, sp.santapp_prefix_decode_attn(geom, k, v, q, ks, vs, lens))
 
 
-def test_large_logits_and_sharp_rows():
-    B, N = 4, 3000
-    geom, q, k, v, ks, vs, lens = inputs(B, 28, 4, N, 30, "bf16", 3)
-    k = (k.float() * torch.linspace(0.1, 10, N, device="cuda")[None, :, None]).to(torch.bfloat16)
+@pytest.mark.parametrize("B,elem", [(2, "bf16"), (4, "fp16"), (40, "bf16"), (40, "fp16")])
+@pytest.mark.parametrize("most", [3, 10, 50])
+def test_large_logits_and_sharp_rows(B, elem, most):
+    N = 3000
+    geom, q, k, v, ks, vs, lens = inputs(B, 28, 4, N, 30, elem, 3)
+    k = (k.float() * torch.linspace(0.1, most, N, device="cuda")[None, :, None]).to(k.dtype)
     out = sp.santapp_prefix_decode_attn(geom, k, v, q, ks, vs, lens)
     want, tol = ref.prefix_decode(k, v, None, q, ks, vs, lens.tolist(), 1 / math.sqrt(D))
     ref.close_32(out, want, tol)
+
+
+def test_capped_scores_of_every_size():
+    for scale in (0.01, 0.06, 0.09, 0.5, 4.0):
+        check(3, 8, 2, 700, 20, "bf16", 2.0, scale=scale)
+        check(40, 8, 2, 700, 20, "fp16", 2.0, True, scale=scale)
+
+
+def test_sequences_do_not_touch_one_another():
+    """A query that is not a number spoils its own heads alone."""
+    B, N = 6, 900
+    geom, q, k, v, ks, vs, lens = inputs(B, 12, 4, N, 16, "bf16", 17)
+    want = sp.santapp_prefix_decode_attn(geom, k, v, q, ks, vs, lens)
+    q[2, 5] = float("nan")
+    got = sp.santapp_prefix_decode_attn(geom, k, v, q, ks, vs, lens)
+    assert bool(torch.isnan(got[2, 5]).all())
+    got[2, 5] = want[2, 5]
+    assert torch.equal(got, want)
+
+
+def test_a_given_stream():
+    B, N = 3, 600
+    geom, q, k, v, ks, vs, lens = inputs(B, 8, 2, N, 16, "bf16", 19)
+    want = sp.santapp_prefix_decode_attn(geom, k, v, q, ks, vs, lens)
+    s = torch.cuda.Stream()
+    out, ws = torch.zeros_like(want), torch.empty(sp.santapp_prefix_decode_workspace_bytes(geom, N, 16), dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
+    sp.santapp_prefix_decode_attn(geom, k, v, q, ks, vs, lens, out=out, workspace=ws, stream=s)
+    s.synchronize()
+    assert torch.equal(out, want)
 
 
 def test_offsets_past_32_bits():

@@ -89,11 +89,13 @@ def test_other_sequences_reach_nothing():
     assert torch.equal(got[100:230], want[100:230])
 
 
-def test_large_logits_and_sharp_rows():
-    """Scores far apart, growing along the row, so the running maximum moves often and far."""
+@pytest.mark.parametrize("elem", ["bf16", "fp16"])
+@pytest.mark.parametrize("most", [3, 12, 60])
+def test_large_logits_and_sharp_rows(elem, most):
+    """Scores far apart, growing along the row, so the running maximum moves often and far (or a little and often)."""
     n = 700
-    geom, q, k, v = inputs([n], [n], 8, 2, "bf16", 5)
-    k = (k.float() * torch.linspace(0.1, 12, n, device="cuda")[None, :, None]).to(torch.bfloat16)
+    geom, q, k, v = inputs([n], [n], 8, 2, elem, 5)
+    k = (k.float() * torch.linspace(0.1, most, n, device="cuda")[None, :, None]).to(k.dtype)
     out = sp.santapp_prompt_attn(geom, [n], q, k, v)
     want, tol = ref.prompt(q, k, v, [n], [n], [0], 1 / math.sqrt(D))
     ref.close_16(out, want, tol)
@@ -106,6 +108,27 @@ def test_values_at_the_type_s_edge():
     out = sp.santapp_prompt_attn(geom, [n], q, k, v)
     want, tol = ref.prompt(q, k, v, [n], [n], [0], 1 / math.sqrt(D))
     ref.close_16(out, want, tol)
+
+
+def test_capped_scores_of_every_size():
+    """Logits far inside the cap, about it and far beyond it: the three ways a tile's tanh is taken."""
+    for scale in (0.01, 0.06, 0.09, 0.5, 4.0):
+        check([300], 8, 2, "bf16", cap=2.0, scale=scale)
+        check([300], 8, 2, "fp16", cap=2.0, scale=scale, bias=True)
+
+
+def test_rows_that_see_infinities_and_zeros():
+    """A key of zeros weighs like any other; an infinite value reaches exactly the queries behind it."""
+    n = 260
+    geom, q, k, v = inputs([n], [n], 4, 4, "bf16", 31)
+    k[:, 5], q[7] = 0, 0
+    v[:, 200] = float("inf")
+    out = sp.santapp_prompt_attn(geom, [n], q, k, v)
+    v2 = v.clone()
+    v2[:, 200] = 0
+    want, tol = ref.prompt(q, k, v2, [n], [n], [0], 1 / math.sqrt(D))
+    ref.close_16(out[:128], want[:128], tol[:128])       # (queries 128 .. 199 share a tile of keys with row 200, as the header says)
+    assert not bool(torch.isfinite(out[200:]).any())
 
 
 def test_runs_are_alike_and_captured_ones_too():

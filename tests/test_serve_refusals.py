@@ -74,7 +74,7 @@ def test_fork_refuses(lib, kw, want):
 @pytest.mark.parametrize("kw,want", [(dict(k=None), BAD), (dict(v=None), BAD), (dict(k=A + 8), BAD), (dict(N=-1), BAD), (dict(plane=99), BAD),
                                      (dict(tok=A + 2), BAD), (dict(q=None), BAD), (dict(out=A + 4), BAD), (dict(ws=None), BAD), (dict(size=64), SMALL),
                                      (dict(cap=-1), BAD), (dict(ks=None), BAD), (dict(o=dict(scale=-1.0)), BAD), (dict(o=dict(scale=math.nan)), BAD),
-                                     (dict(o=dict(cap=-1.0)), BAD), (dict(o=dict(cap=math.inf)), BAD), (dict(o=dict(slopes=A + 1)), BAD),
+                                     (dict(o=dict(cap=-1.0)), BAD), (dict(o=dict(cap=math.inf)), BAD), (dict(o=dict(cap=1e-42)), BAD), (dict(o=dict(slopes=A + 1)), BAD),
                                      (dict(o=dict(status=A + 2)), BAD), (dict(N=2 ** 30, plane=2 ** 30), NO), (dict(plane=2 ** 31), NO),
                                      (dict(B=70000), NO), (dict(cap=2 ** 29), NO)])
 def test_prefix_refuses(lib, kw, want):
