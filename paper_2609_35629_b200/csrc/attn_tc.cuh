@@ -245,7 +245,8 @@ __device__ __forceinline__ int ta_group(const TaItem &it, int place) { return it
 __device__ __forceinline__ bool ta_cut(const TaItem &it) { return it.fix_tail && it.n_keys < (it.tile0 + ta_tiles(it)) * kTaTile; }
 
 // cap * tanh(x cap_in) * log2 e of a thread's products: tanh(y) = y P(y^2) with the P of kN coefficients that has the smallest largest relative
-// error on [0, 1/2] (kWide: [0, 1]), cap * log2 e folded into them: 5e-7 of 4 coefficients, 1e-8 of 5 (kWide 6e-7 of 6, 5e-8 of 7).
+// error on [0, 1/2] (kWide: [0, 1]), cap * log2 e folded into them: 5e-7 of 4 coefficients, 1e-8 of 5 (kWide 6e-7 of 6, 5e-8 of 7). On
+// [0, 1/2] the powers of cap_in are folded into them too, which leaves the squares of the products themselves: one multiplication less.
 template <bool kWide, int kN, int kCols>
 __device__ __forceinline__ void ta_cap_poly(const TaScore &sc, float (&v)[kCols])
 {
@@ -257,14 +258,21 @@ __device__ __forceinline__ void ta_cap_poly(const TaScore &sc, float (&v)[kCols]
                                  -0.006203379104680566f, 0.0010410226337084262f}};
     static_assert(kWide ? kN == 6 || kN == 7 : kN == 4 || kN == 5, "a row of the table");
     uint64_t c[kN];
+    float by = kWide ? sc.cap_log2 : sc.cap_log2 * sc.cap_in;
 #pragma unroll
-    for (int k = 0; k < kN; ++k) c[k] = ta_two(kP[kN - 4][k] * sc.cap_log2, kP[kN - 4][k] * sc.cap_log2);
+    for (int k = 0; k < kN; ++k) {
+        c[k] = ta_two(kP[kN - 4][k] * by, kP[kN - 4][k] * by);
+        if (!kWide) by *= sc.cap_in * sc.cap_in;
+    }
     const uint64_t in = ta_two(sc.cap_in, sc.cap_in);
 #pragma unroll
     for (int i = 0; i < kCols; i += 8) {                    // four pairs side by side: one alone waits for each of its products
         uint64_t y[4], u[4], r[4];
 #pragma unroll
-        for (int x = 0; x < 4; ++x) y[x] = ta_mul2(ta_two(v[i + 2 * x], v[i + 2 * x + 1]), in);
+        for (int x = 0; x < 4; ++x) {
+            y[x] = ta_two(v[i + 2 * x], v[i + 2 * x + 1]);
+            if (kWide) y[x] = ta_mul2(y[x], in);
+        }
 #pragma unroll
         for (int x = 0; x < 4; ++x) u[x] = ta_mul2(y[x], y[x]);
 #pragma unroll
@@ -288,7 +296,8 @@ __device__ __forceinline__ void ta_cap(const TaScore &sc, float (&v)[kCols])
 #pragma unroll
         for (int x = 0; x < 4; ++x) most[x] = fmaxf(fmaxf(most[x], fabsf(v[i + x])), fabsf(v[i + 4 + x]));
     const float far = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3])) * sc.cap_in;
-    if (__all_sync(0xFFFFFFFFu, far <= 0.5f)) {
+    // (cap_in within 2^-12 and 2^12: its eighth power is a normal number)
+    if (sc.cap_in >= 0x1p-12f && sc.cap_in <= 0x1p12f && __all_sync(0xFFFFFFFFu, far <= 0.5f)) {
         ta_cap_poly<false, kTwo ? 5 : 4>(sc, v);
     } else if (__all_sync(0xFFFFFFFFu, far <= 1.f)) {
         ta_cap_poly<true, kTwo ? 7 : 6>(sc, v);
