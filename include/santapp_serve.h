@@ -16,7 +16,8 @@
  * buffers, workspaces that need no initialisation, asynchronous on `stream`, nothing kept between
  * calls, negative santapp_status on error, argument errors found on the host before any launch.
  * Of santapp_geom the calls use n_seqs, the head counts, head_dim and elem_type (the parent fields
- * only have to be valid). Every call may be captured into a CUDA graph and replayed.
+ * only have to be valid). Every call may be captured into a CUDA graph and replayed, and
+ * santapp_last_launch_count tells how many kernels it launched.
  */
 #ifndef SANTAPP_SERVE_H
 #define SANTAPP_SERVE_H

@@ -88,6 +88,33 @@ def test_lengths_are_clamped_and_rows_may_be_empty():
     check(2, 8, 2, 0, 0)
 
 
+def test_a_large_batch():
+    check(300, 8, 2, 260, 5)
+
+
+def test_no_lengths_are_no_suffix():
+    geom, q, k, v, ks, vs, lens = inputs(3, 8, 2, 300, 16, "bf16", 23)
+    got = sp.santapp_prefix_decode_attn(geom, k, v, q, ks, vs, None)
+    assert torch.equal(got, sp.santapp_prefix_decode_attn(geom, k, v, q, None, None, None))
+
+
+def test_a_first_call_may_be_captured():
+    """Set-up that a kernel needs once (shared memory beyond the default) is no work on the stream."""
+    B, N = 2, 200
+    geom, q, k, v, ks, vs, lens = inputs(B, 12, 12, N, 8, "fp16", 29)
+    slopes = slopes_of(12)
+    out = torch.zeros(B, 12, D, device="cuda")
+    ws = torch.empty(sp.santapp_prefix_decode_workspace_bytes(geom, N, 8), dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        sp.santapp_prefix_decode_attn(geom, k, v, q, ks, vs, lens, cap=9.0, slopes=slopes, out=out, workspace=ws)
+    graph.replay()
+    torch.cuda.synchronize()
+    want, tol = ref.prefix_decode(k, v, None, q, ks, vs, lens.tolist(), 1 / math.sqrt(D), 9.0, slopes)
+    ref.close_32(out, want, tol)
+
+
 def test_scale():
     check(2, 8, 2, 400, 8, scale=0.21)
 

@@ -50,6 +50,31 @@ def test_append_rotates_and_writes_one_row(kw, elem, n, hq, hkv):
     assert torch.equal(out[..., rot:], q[..., rot:]), "values past rot_dim are copied"
 
 
+def test_append_for_a_very_large_batch():
+    """Several tokens a block, the last block not full, lengths in place, some slots padded."""
+    n, cap = 2501, 3
+    geom, rope = geometry(n, 4, 2, "bf16"), sp.Rope(rot_dim=32)
+    q, k, v = qkv(n, 4, 2, geom.torch_dtype, 2)
+    lens = torch.arange(n, dtype=torch.int32, device="cuda") % 5 - 1
+    base = torch.arange(n, dtype=torch.int32, device="cuda") * 7
+    ks = torch.zeros(n, 2, cap, D, dtype=geom.torch_dtype, device="cuda")
+    vs = torch.zeros_like(ks)
+    n0 = lens.clone()
+    out = sp.santapp_rope_append(geom, rope, q, k, v, base, lens, ks, vs, suffix_len_out=lens)
+    live = (n0 >= 0) & (n0 < cap)
+    assert torch.equal(lens, torch.where(live, n0 + 1, n0))
+    b = live.nonzero()[:, 0]
+    at = n0[b].long()
+    want, off = ref.rotate(rope, q[b], base[b].long() + at, False)
+    ref.close_16(out[b], want, off, "q")
+    want, off = ref.rotate(rope, k[b], base[b].long() + at, False)
+    ref.close_16(ks[b, :, at], want, off, "k")
+    assert torch.equal(vs[b, :, at], v[b])
+    written = torch.zeros(n, cap, dtype=torch.bool, device="cuda")
+    written[b, at] = True
+    assert not bool(ks.transpose(1, 2)[~written].any()) and not bool(vs.transpose(1, 2)[~written].any())
+
+
 def test_append_in_place_and_lengths_in_place():
     geom, rope = geometry(6, 28, 4, "bf16"), sp.Rope()
     q, k, v = (x.contiguous() for x in qkv(6, 28, 4, geom.torch_dtype))
