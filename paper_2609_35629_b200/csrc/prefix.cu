@@ -299,7 +299,9 @@ finish_kernel(const __grid_constant__ PrefixParams p)
 #pragma unroll
             for (int h = 0; h < kMaxGroup; ++h) {
                 const float mm = __shfl_sync(0xFFFFFFFFu, ml_now.x, h), ll = __shfl_sync(0xFFFFFFFFu, ml_now.y, h);
-                if (h >= G || mm == -CUDART_INF_F) continue;
+                // (a part whose scores are all no numbers has no maximum either, but its sum is none: it is taken, and the factors
+                // exp2(-inf - -inf), or 0 times it, leave no number)
+                if (h >= G || (mm == -CUDART_INF_F && ll == 0.f)) continue;
                 const float t = fmaxf(top[h], mm), a = ta_ex2(top[h] - t), w = ta_ex2(mm - t);
                 top[h] = t;
                 sum[h] = fmaf(w, ll, sum[h] * a);
