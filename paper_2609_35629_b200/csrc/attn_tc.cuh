@@ -247,8 +247,8 @@ __device__ __forceinline__ bool ta_cut(const TaItem &it) { return it.fix_tail &&
 // cap * tanh(x cap_in) * log2 e of a thread's products: tanh(y) = y P(y^2) with the P of kN coefficients that has the smallest largest relative
 // error on [0, 1/2] (kWide: [0, 1]), cap * log2 e folded into them: 5e-7 of 4 coefficients, 1e-8 of 5 (kWide 6e-7 of 6, 5e-8 of 7). On
 // [0, 1/2] the powers of cap_in are folded into them too, which leaves the squares of the products themselves: one multiplication less.
-template <bool kWide, int kN, int kCols>
-__device__ __forceinline__ void ta_cap_poly(const TaScore &sc, float (&v)[kCols])
+template <int kN>
+__device__ __forceinline__ constexpr float ta_tanh_term(int k)
 {
     constexpr float kP[4][7] = {{0.9999994557709386f, -0.33326317935941724f, 0.13190296603213952f, -0.04440222612781058f},
                                 {0.9999999868718333f, -0.33333069394022213f, 0.1332477931761862f, -0.05298607529180707f, 0.0171350066346453f},
@@ -256,12 +256,28 @@ __device__ __forceinline__ void ta_cap_poly(const TaScore &sc, float (&v)[kCols]
                                  -0.0030670603265534825f},
                                 {0.9999999502407364f, -0.3333283915307065f, 0.1332520407582405f, -0.0534570295681808f, 0.02028998042301148f,
                                  -0.006203379104680566f, 0.0010410226337084262f}};
+    return kP[kN - 4][k];
+}
+// cap_log2 * tanh(y) of one value: the polynomial up to 1, beyond it from e = exp(-2 |y|) as (1 - e) / (1 + e), which would cancel for small y (its error
+// is 2^-22 of the cap, whatever the score: a cap of 1e6 left scores of 1 nothing).
+template <int kN>
+__device__ __forceinline__ float ta_cap_one(float y, float cap_log2)
+{
+    const float u = y * y, e = ta_ex2(-2.885390082f * fabsf(y));
+    float r = ta_tanh_term<kN>(kN - 1);
+#pragma unroll
+    for (int k = kN - 2; k >= 0; --k) r = fmaf(r, u, ta_tanh_term<kN>(k));
+    return (fabsf(y) <= 1.f ? r * y : copysignf(__fdividef(1.f - e, 1.f + e), y)) * cap_log2;
+}
+template <bool kWide, int kN, int kCols>
+__device__ __forceinline__ void ta_cap_poly(const TaScore &sc, float (&v)[kCols])
+{
     static_assert(kWide ? kN == 6 || kN == 7 : kN == 4 || kN == 5, "a row of the table");
     uint64_t c[kN];
     float by = kWide ? sc.cap_log2 : sc.cap_log2 * sc.cap_in;
 #pragma unroll
     for (int k = 0; k < kN; ++k) {
-        c[k] = ta_two(kP[kN - 4][k] * by, kP[kN - 4][k] * by);
+        c[k] = ta_two(ta_tanh_term<kN>(k) * by, ta_tanh_term<kN>(k) * by);
         if (!kWide) by *= sc.cap_in * sc.cap_in;
     }
     const uint64_t in = ta_two(sc.cap_in, sc.cap_in);

@@ -221,8 +221,7 @@ finish_kernel(const __grid_constant__ PrefixParams p)
         for (int i = 0; i < 4; ++i) {
             const int key = blk * kFinishBlock + kc + (i & 1) + (i >> 1) * 8;
             if constexpr (kCap) {
-                const float x = v[i] * p.score.cap_in, e = ta_ex2(-2.885390082f * fabsf(x));
-                v[i] = copysignf(__fdividef(1.f - e, 1.f + e), x) * p.score.cap_log2;
+                v[i] = ta_cap_one<7>(v[i] * p.score.cap_in, p.score.cap_log2);
             } else {
                 v[i] *= p.score.scale_log2;
             }
