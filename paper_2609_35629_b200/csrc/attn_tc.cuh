@@ -301,10 +301,37 @@ __device__ __forceinline__ void ta_cap_poly(const TaScore &sc, float (&v)[kCols]
         for (int x = 0; x < 4; ++x) ta_split(ta_mul2(r[x], y[x]), v[i + 2 * x], v[i + 2 * x + 1]);
     }
 }
-// By a polynomial where the warp's |x cap_in| are at most 1, the usual case. Otherwise from e = exp(-2 |y|): (1 - e) / (1 + e) with y's sign,
-// two uses of the special-function unit.
+// The same where scores reach beyond the cap: the polynomial (of kN coefficients) up to |y| = 1/2, and from there on (1 - e) / (1 + e) with
+// e = exp(-2 |y|), two uses of the special-function unit, good to 2^-21 there. (Below, it cancels: 2^-22 of the cap would be left of small
+// scores that stand beside large ones.)
+template <int kN>
+__device__ __forceinline__ void ta_cap_far(const TaScore &sc, float (&v)[32])
+{
+    static_assert(kN == 4 || kN == 5, "a row of the table");
+    const uint64_t in = ta_two(sc.cap_in, sc.cap_in);
+    uint64_t c[kN];
+#pragma unroll
+    for (int k = 0; k < kN; ++k) c[k] = ta_two(ta_tanh_term<kN>(k) * sc.cap_log2, ta_tanh_term<kN>(k) * sc.cap_log2);
+#pragma unroll
+    for (int i = 0; i < 32; i += 2) {
+        const uint64_t y = ta_mul2(ta_two(v[i], v[i + 1]), in), u = ta_mul2(y, y);
+        uint64_t r = c[kN - 1];
+#pragma unroll
+        for (int k = kN - 2; k >= 0; --k) r = ta_fma2(r, u, c[k]);
+        float near[2], at[2];
+        ta_split(ta_mul2(r, y), near[0], near[1]);
+        ta_split(y, at[0], at[1]);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const float e = ta_ex2(-2.885390082f * fabsf(at[h])), far = copysignf(__fdividef(1.f - e, 1.f + e), at[h]) * sc.cap_log2;
+            v[i + h] = fabsf(at[h]) <= 0.5f ? near[h] : far;
+        }
+    }
+}
+// By a polynomial where the warp's |x cap_in| are at most 1, the usual case. Otherwise 32 of the thread's columns (from t_v on in tensor memory) at a time,
+// there and back, which keeps that path's code short: unrolled over all of them it cost the others 3 to 10 %.
 template <bool kTwo, int kCols>
-__device__ __forceinline__ void ta_cap(const TaScore &sc, float (&v)[kCols])
+__device__ __forceinline__ void ta_cap(const TaScore &sc, uint32_t t_v, float (&v)[kCols])
 {
     float most[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -318,11 +345,21 @@ __device__ __forceinline__ void ta_cap(const TaScore &sc, float (&v)[kCols])
     } else if (__all_sync(0xFFFFFFFFu, far <= 1.f)) {
         ta_cap_poly<true, kTwo ? 7 : 6>(sc, v);
     } else {
-#pragma unroll
-        for (int i = 0; i < kCols; ++i) {
-            const float y = v[i] * sc.cap_in, e = ta_ex2(-2.885390082f * fabsf(y));
-            v[i] = copysignf(__fdividef(1.f - e, 1.f + e), y) * sc.cap_log2;
+#pragma unroll 1
+        for (int q = 0; q < kCols / 32; ++q) {
+            float w[32];
+            ta_ld32(t_v + 32 * q, w);
+            ta_ld_wait();
+            ta_tie(w);
+            ta_cap_far<kTwo ? 5 : 4>(sc, w);
+            ta_st32(t_v + 32 * q, w);
         }
+        ta_st_wait();
+#pragma unroll
+        for (int q = 0; q < kCols / 32; ++q) ta_ld32(t_v + 32 * q, v + 32 * q);
+        ta_ld_wait();
+#pragma unroll
+        for (int q = 0; q < kCols / 32; ++q) ta_tie(v + 32 * q);
     }
 }
 
@@ -369,7 +406,7 @@ __device__ __forceinline__ bool ta_softmax(TaSmem &sm, const TaItem &it, const T
             ta_ld_wait();
 #pragma unroll
             for (int q = 0; q < kCols / 32; ++q) ta_tie(v + 32 * q);
-            if constexpr (kCap) ta_cap<kTwo>(sc, v);
+            if constexpr (kCap) ta_cap<kTwo>(sc, t_s + col0, v);
             if constexpr (kBias) {
                 // linear in the key's position as long as no key is behind the query
                 const bool table = key_pos != nullptr;

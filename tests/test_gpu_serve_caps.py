@@ -17,10 +17,10 @@ def rand(*shape, seed=0, dtype=torch.bfloat16):
 
 
 def capped(q, k, v, seen, scale, cap, weight_off):
-    """One head, as ref.attend has it, but for the cap's own error: below 2^-20 of the capped score. With y = s / cap (its factor and its product
-    rounded: 2^-23 of y, so at most that of tanh y): below 1 a polynomial good to 2^-20.6, beyond it (1 - e) / (1 + e) with e = exp(-2 |y|)
-    < 0.136 to 2^-20 (2^-22 of the instruction, and 2^-24 * 2.9 |y| e of its argument), which moves it by 2 * 0.136 * 2^-20; a
-    quotient to 2^-22. The sums of these are below 2^-19.9."""
+    """One head, as ref.attend has it, but for the cap's own error: below 2^-19.9 of the capped score. With y = s / cap (its factor and its product
+    rounded: 2^-23 of y, so at most that of tanh y): near zero a polynomial good to 2^-20.6, beyond it (1 - e) / (1 + e) with e = exp(-2 |y|) <= 0.37
+    to 2^-21.6 of itself (2^-22 of the instruction, 2^-24 of its argument of at least 1.44), which moves it by 2 e / (1 - e^2) <= 0.86 of that; a
+    quotient to 2^-22 and two products to 2^-24."""
     q, k, v = q.double(), k.double(), v.double()
     s = (q @ k.T) * scale
     raw = 136 * 2.0 ** -23 * (q.abs() @ k.abs().T) * scale
@@ -54,3 +54,26 @@ def test_a_large_cap_leaves_the_suffix_its_scores(cap, B, N, elem):
             kk, vv = torch.cat([k[j], ks[b, j]]), torch.cat([v[j], vs[b, j]])
             want, tol = capped(q[b, h][None], kk, vv, torch.ones(1, len(kk), dtype=torch.bool, device="cuda"), 1 / math.sqrt(D), cap, 2.0 ** -16)
             ref.close_32(got[b, h], want[0], tol[0], f"sequence {b} head {h}")
+
+
+@pytest.mark.parametrize("cap", [1e4, 1e6])
+def test_small_scores_beside_scores_beyond_the_cap(cap):
+    """Rows whose scores are small stand in one block with rows whose scores are several times the cap."""
+    n, hq, hkv = 200, 4, 2
+    geom = sp.Geometry(1, hq, hkv)
+    q, k, v = 3 * rand(n, hq, D), rand(hkv, n, D, seed=1), rand(hkv, n, D, seed=2)
+    q[::7] *= 4 * cap / 3
+    got = sp.santapp_prompt_attn(geom, [n], q, k, v, cap=cap)
+    seen = torch.ones(n, n, dtype=torch.bool, device="cuda").tril()
+    small = torch.arange(n, device="cuda") % 7 != 0
+    for h in range(hq):
+        want, tol = capped(q[:, h], k[h // 2], v[h // 2], seen, 1 / math.sqrt(D), cap, 2.0 ** -8 + 2.0 ** -17)
+        ref.close_16(got[small, h], want[small], tol[small], f"head {h}")
+    B = 8
+    gq = 3 * rand(B, 8, D, seed=5)
+    gq[::2] *= 4 * cap / 3
+    one = sp.santapp_prefix_decode_attn(sp.Geometry(B, 8, hkv), k, v, gq, None, None, None, cap=cap)
+    for b in range(1, B, 2):
+        for h in range(8):
+            want, tol = capped(gq[b, h][None], k[h // 4], v[h // 4], torch.ones(1, n, dtype=torch.bool, device="cuda"), 1 / math.sqrt(D), cap, 2.0 ** -16)
+            ref.close_32(one[b, h], want[0], tol[0], f"sequence {b} head {h}")
