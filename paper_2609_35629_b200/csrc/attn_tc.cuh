@@ -35,7 +35,7 @@
 namespace santapp {
 
 constexpr int kTaThreads = 384;           // warps 0-3, 4-7: a row per thread of streams 0, 1; warp 8: copies; warp 9: products; warp 10: the
-                                          // last tile's rows that are somebody else's
+                                          // last tile's values that are somebody else's; warp 11: its keys, where scores are capped
 constexpr int kTaTile = 128;              // query rows of a stream, keys of a tile
 constexpr int kTaTileBytes = kTaTile * kHeadDim * 2;
 constexpr int kTaRing = 5;                // tiles of keys or values under way
@@ -47,7 +47,7 @@ struct TaSmem {
     unsigned char ring[kTaRing][kTaTileBytes];
     uint64_t full[4], left[4];                // a group of tiles has landed; the products have left it. By group % 4
     uint64_t q_ready, s_ready[2], p_ready[2][2], done[2];      // p_ready: weights of keys 0-95, 96-127
-    uint64_t pos_ready[2][2], tail;           // tail: the last tile of values has landed, with somebody else's rows behind it
+    uint64_t pos_ready[2][2], tail[2];        // tail: the last tile of keys (0), of values (1) has landed, with somebody else's rows behind it
     alignas(16) float pos[2][2][kTaTile];                 // positions of the keys of a stream's tile, less n_keys; by tile parity
     uint32_t tmem;
     int failed;
@@ -74,7 +74,8 @@ struct TaItem {
     int count0, count1;       // key tiles of each stream
     bool shared;              // the streams are two row tiles over the same keys
     int fold;                 // not shared: the 128 lanes hold the rows 1, 2 or 4 times, each time for another part of a tile's keys
-    bool fix_tail;            // the planes hold rows behind n_keys: they are zeroed in V's last tile (0 times NaN is no 0)
+    bool fix_tail;            // the planes hold rows behind n_keys: they are zeroed in V's last tile (0 times NaN is no 0), and with a cap
+                              // in K's (how the warp takes its tanh goes by the largest score of the tile, seen or not)
 };
 struct TaScore {
     float scale_log2;         // scale * log2 e
@@ -559,7 +560,7 @@ __device__ __forceinline__ void ta_block(TaSmem &sm, const TaItem &it, const TaS
             asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(ta_addr(&sm.left[i])), "r"(1));
         }
         asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(ta_addr(&sm.q_ready)), "r"(256));
-        asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(ta_addr(&sm.tail)), "r"(1));
+        for (int i = 0; i < 2; ++i) asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(ta_addr(&sm.tail[i])), "r"(1));
         for (int s = 0; s < 2; ++s) {
             asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(ta_addr(&sm.s_ready[s])), "r"(1));
             for (int i = 0; i < 2; ++i) asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(ta_addr(&sm.p_ready[s][i])), "r"(4));
@@ -606,8 +607,9 @@ __device__ __forceinline__ void ta_block(TaSmem &sm, const TaItem &it, const TaS
                         if (g > waited && !ta_wait(sm, &sm.left[g & 3], (uint32_t)(g >> 2) & 1u)) return false;
                         waited = g;
                     }
-                    // (warp 10 hands on a tile of values that ends in somebody else's rows)
-                    const uint32_t bar = ta_addr(value && cut && tile == n_tiles - 1 ? &sm.tail : &sm.full[group & 3]), dst = ta_addr(sm.ring[n % kTaRing]);
+                    // (warps 10 and 11 hand on tiles that end in somebody else's rows)
+                    const bool fixed = cut && tile == n_tiles - 1 && (value || kCap);
+                    const uint32_t bar = ta_addr(fixed ? &sm.tail[value] : &sm.full[group & 3]), dst = ta_addr(sm.ring[n % kTaRing]);
                     const int y = it.key0 + (it.tile0 + tile) * kTaTile;
                     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(kTaTileBytes) : "memory");
                     const CUtensorMap *map = value ? v_map : k_map;
@@ -706,14 +708,16 @@ __device__ __forceinline__ void ta_block(TaSmem &sm, const TaItem &it, const TaS
                 }
             }
             __syncwarp();
-        } else if (warp == 10 && ta_cut(it)) {
-            // ---- the rows behind the last one, in the last tile of values ----
-            const int place = 2 * ta_tiles(it) - 1, valid = it.n_keys - (it.tile0 + ta_tiles(it) - 1) * kTaTile;
-            if (ta_wait_warp(sm, &sm.tail, 0)) {
+        } else if (ta_cut(it) && (warp == 10 || kCap)) {
+            // ---- the rows behind the last one, in the last tile of values (warp 10) and of keys ----
+            const bool value = warp == 10;
+            const int last = ta_tiles(it) - 1, valid = it.n_keys - (it.tile0 + last) * kTaTile;
+            const int place = value ? 2 * last + 1 : ta_key_place(it, last), group = value ? last + 1 : ta_group(it, place);
+            if (ta_wait_warp(sm, &sm.tail[value], 0)) {
                 for (int e = max(valid, 0) * 16 + lane; e < kTaTile * 16; e += 32)
                     *reinterpret_cast<uint4 *>(sm.ring[place % kTaRing] + ta_byte(e >> 4, e & 15)) = make_uint4(0, 0, 0, 0);
                 proxy_fence();
-                ta_arrive_warp(&sm.full[ta_tiles(it) & 3]);          // (the last group is this tile's)
+                ta_arrive_warp(&sm.full[group & 3]);
             }
         }
     }
