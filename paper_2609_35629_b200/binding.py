@@ -6,8 +6,10 @@ streams. There is no CPU fallback: if the library is missing or cannot be loaded
 the first call raises.
 
 The functions keep the names of the C entry points (include/santapp.h, include/santapp_latent.h,
-include/santapp_serve.h).
+include/santapp_serve.h). With `stream=s` a call runs on s; outputs and workspaces that it makes itself are
+that stream's memory, and the current stream may use the outputs once it has waited for s.
 """
+import contextlib
 import ctypes
 import functools
 import os
@@ -228,6 +230,33 @@ def _stream_ptr(stream):
     return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
 
 
+def _on(stream):
+    """Where a call's buffers are made: on the stream it runs on (None: the current one). Memory that belonged to another stream could
+    still be in use there when the call starts, or be given to somebody else on it while the call is under way."""
+    if stream is None:
+        return contextlib.nullcontext()
+    return torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(stream.cuda_stream))
+
+
+def _handed_out(stream, *tensors):
+    """Buffers of a given stream that the caller gets: the current stream may use them too, until they are dropped."""
+    if stream is not None:
+        for t in tensors:
+            if t.is_cuda:
+                t.record_stream(torch.cuda.current_stream(t.device))
+
+
+def _empty(shape, dtype, device, stream, handed_out=True):
+    """A buffer made for a call on `stream`: one that the caller gets, or a workspace."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with _on(stream):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    if handed_out:
+        _handed_out(stream, t)
+    return t
+
+
 @functools.lru_cache(maxsize=256)
 def _geom_ref(cls, *fields):
     """Reference to a geometry struct (read only, kept for the next call with the same fields)."""
@@ -289,6 +318,9 @@ class Teams:
                         self.seq_row_off.data_ptr(), self.seq_team_off.data_ptr(), self.rep_abs_max.data_ptr(),
                         self.team_count.data_ptr(), sizes.rows_total, sizes.teams_total, sizes.max_teams_per_seq, sizes.max_rows_per_seq)
 
+    def tensors(self):
+        return [x for x in vars(self).values() if isinstance(x, torch.Tensor)]
+
 
 def santapp_version() -> int:
     return load_library().santapp_version()
@@ -324,8 +356,10 @@ def santapp_build_teams(geom: Geometry, prompt_len, k_prompt: torch.Tensor, v_pr
     """k_prompt, v_prompt: bf16 CUDA tensors [n_kv_heads, rows_total, d] in token order."""
     L = load_library()
     sizes = santapp_build_teams_sizes(geom, prompt_len)
-    teams = Teams(geom, sizes, k_prompt.device)
-    ws = torch.empty(max(sizes.build_workspace_bytes, 256), dtype=torch.uint8, device=k_prompt.device)
+    with _on(stream):
+        teams = Teams(geom, sizes, k_prompt.device)
+        ws = torch.empty(max(sizes.build_workspace_bytes, 256), dtype=torch.uint8, device=k_prompt.device)
+    _handed_out(stream, *teams.tensors())
     n = len(prompt_len)
     arr = (ctypes.c_int32 * n)(*[int(x) for x in prompt_len])
     _check(getattr(L, _entry)(geom.ref(), arr, _ptr(k_prompt), _ptr(v_prompt), ctypes.byref(teams.c),
@@ -356,9 +390,11 @@ def santapp_kmeans_fit(geom: Geometry, prompt_len, n_centres, k_prompt: torch.Te
     if need == 0:
         raise SantappError(SANTAPP_ERR_INVALID_ARG, "k-means fit arguments")
     dev = k_prompt.device
-    ws = torch.empty(need, dtype=torch.uint8, device=dev)
-    centres = torch.empty((geom.n_kv_heads, int(sum(n_centres)), geom.head_dim), dtype=torch.float32, device=dev)
-    steps = torch.zeros((geom.n_kv_heads, geom.n_seqs), dtype=torch.int32, device=dev)
+    with _on(stream):
+        ws = torch.empty(need, dtype=torch.uint8, device=dev)
+        centres = torch.empty((geom.n_kv_heads, int(sum(n_centres)), geom.head_dim), dtype=torch.float32, device=dev)
+        steps = torch.zeros((geom.n_kv_heads, geom.n_seqs), dtype=torch.int32, device=dev)
+    _handed_out(stream, centres, steps)
     _check(L.santapp_kmeans_fit(geom.ref(), n, c, _ptr(k_prompt), ctypes.byref(o), _ptr(centres), _ptr(steps),
                                 _ptr(ws), ws.numel(), _stream_ptr(stream)))
     centres._ws = ws
@@ -372,9 +408,11 @@ def santapp_assign_parents(geom: Geometry, prompt_len, n_centres, k_prompt: torc
     L = load_library()
     if centres.dtype != torch.float32:
         raise SantappError(SANTAPP_ERR_INVALID_ARG, "centres must be float32")
-    parent_of = torch.empty((geom.n_kv_heads, k_prompt.shape[1]), dtype=torch.int32, device=k_prompt.device)
-    ws = torch.empty(max(int(L.santapp_assign_parents_workspace_bytes(geom.ref())), 256), dtype=torch.uint8,
-                     device=k_prompt.device)
+    with _on(stream):
+        parent_of = torch.empty((geom.n_kv_heads, k_prompt.shape[1]), dtype=torch.int32, device=k_prompt.device)
+        ws = torch.empty(max(int(L.santapp_assign_parents_workspace_bytes(geom.ref())), 256), dtype=torch.uint8,
+                         device=k_prompt.device)
+    _handed_out(stream, parent_of)
     _check(L.santapp_assign_parents(geom.ref(), _i32_array(prompt_len), _i32_array(n_centres), _ptr(k_prompt),
                                     _ptr(centres), _ptr(parent_of), _ptr(ws), ws.numel(), _stream_ptr(stream)))
     parent_of._ws = ws
@@ -403,8 +441,10 @@ def santapp_build_teams_parents(geom: Geometry, prompt_len, n_parents, k_prompt:
     """Team records from a parent label per token (int32 CUDA tensor [n_kv_heads, rows_total])."""
     L = load_library()
     sizes = santapp_parent_teams_sizes(geom, prompt_len, n_parents)
-    teams = Teams(geom, sizes, k_prompt.device)
-    ws = torch.empty(max(sizes.build_workspace_bytes, 256), dtype=torch.uint8, device=k_prompt.device)
+    with _on(stream):
+        teams = Teams(geom, sizes, k_prompt.device)
+        ws = torch.empty(max(sizes.build_workspace_bytes, 256), dtype=torch.uint8, device=k_prompt.device)
+    _handed_out(stream, *teams.tensors())
     if parent_of.dtype != torch.int32:
         raise SantappError(SANTAPP_ERR_INVALID_ARG, "parent_of must be int32")
     _check(getattr(L, _entry)(geom.ref(), _i32_array(prompt_len), _i32_array(n_parents),
@@ -448,10 +488,9 @@ def santapp_decode_attn(geom: Geometry, teams: Teams, q: torch.Tensor, k_suffix:
     step_dev optional device int32/uint32 [1] added to `step` on the device."""
     L = load_library()
     if out is None:
-        out = torch.empty((geom.n_seqs, geom.n_q_heads, geom.head_dim), dtype=torch.float32, device=q.device)
+        out = _empty((geom.n_seqs, geom.n_q_heads, geom.head_dim), torch.float32, q.device, stream)
     if workspace is None:
-        workspace = torch.empty(santapp_decode_workspace_bytes(geom, teams, n_sample), dtype=torch.uint8,
-                                device=q.device)
+        workspace = _empty(santapp_decode_workspace_bytes(geom, teams, n_sample), torch.uint8, q.device, stream, False)
     cap = 0 if k_suffix is None else int(k_suffix.shape[2])
     _check(L.santapp_decode_attn(geom.ref(), ctypes.byref(teams.c), _ptr(q), _ptr(k_suffix), _ptr(v_suffix),
                                  _ptr(suffix_len), cap, n_sample, int(seed), step, _ptr(step_dev),
@@ -466,9 +505,9 @@ def santapp_dense_decode_attn(geom: Geometry, teams: Teams, q: torch.Tensor, k_s
                               workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     L = load_library()
     if out is None:
-        out = torch.empty((geom.n_seqs, geom.n_q_heads, geom.head_dim), dtype=torch.float32, device=q.device)
+        out = _empty((geom.n_seqs, geom.n_q_heads, geom.head_dim), torch.float32, q.device, stream)
     if workspace is None:
-        workspace = torch.empty(santapp_dense_workspace_bytes(geom, teams), dtype=torch.uint8, device=q.device)
+        workspace = _empty(santapp_dense_workspace_bytes(geom, teams), torch.uint8, q.device, stream, False)
     cap = 0 if k_suffix is None else int(k_suffix.shape[2])
     _check(L.santapp_dense_decode_attn(geom.ref(), ctypes.byref(teams.c), _ptr(q), _ptr(k_suffix),
                                        _ptr(v_suffix), _ptr(suffix_len), cap, scale, _ptr(out), _ptr(workspace),
@@ -488,7 +527,7 @@ def santapp_dense_decode_attn_noalloc(geom: Geometry, teams: Teams, q: torch.Ten
     before any stream capture."""
     L = load_library()
     if out is None:
-        out = torch.empty((geom.n_seqs, geom.n_q_heads, geom.head_dim), dtype=torch.float32, device=q.device)
+        out = _empty((geom.n_seqs, geom.n_q_heads, geom.head_dim), torch.float32, q.device, stream)
     cap = 0 if k_suffix is None else int(k_suffix.shape[2])
     _check(L.santapp_dense_decode_attn_noalloc(geom.ref(), ctypes.byref(teams.c), _ptr(q), _ptr(k_suffix),
                                                _ptr(v_suffix), _ptr(suffix_len), cap, scale, _ptr(out),
@@ -531,6 +570,8 @@ class LatentTeams:
                               self.rep_abs_max.data_ptr(), sizes.rows_total, sizes.teams_total,
                               sizes.max_teams_per_seq, sizes.max_rows_per_seq)
 
+    tensors = Teams.tensors
+
 
 def santapp_latent_sizes(geom: LatentGeometry, prompt_len) -> Sizes:
     L = load_library()
@@ -544,8 +585,10 @@ def santapp_latent_build_teams(geom: LatentGeometry, prompt_len, rows_prompt: to
     """rows_prompt: bf16 CUDA tensor [rows_total, 576] in token order (512 latent values, 64 rotary)."""
     L = load_library()
     sizes = santapp_latent_sizes(geom, prompt_len)
-    teams = LatentTeams(geom, sizes, rows_prompt.device)
-    ws = torch.empty(max(sizes.build_workspace_bytes, 256), dtype=torch.uint8, device=rows_prompt.device)
+    with _on(stream):
+        teams = LatentTeams(geom, sizes, rows_prompt.device)
+        ws = torch.empty(max(sizes.build_workspace_bytes, 256), dtype=torch.uint8, device=rows_prompt.device)
+    _handed_out(stream, *teams.tensors())
     _check(L.santapp_latent_build_teams(geom.ref(), _i32_array(prompt_len), _ptr(rows_prompt), ctypes.byref(teams.c),
                                         _ptr(ws), ws.numel(), _stream_ptr(stream)))
     teams._build_ws = ws
@@ -578,10 +621,9 @@ def santapp_latent_decode_attn(geom: LatentGeometry, teams: LatentTeams, q: torc
     L = load_library()
     cap = 0 if suffix_rows is None else int(suffix_rows.shape[1])
     if out is None:
-        out = torch.empty((geom.n_seqs, geom.n_heads, LATENT_DIM), dtype=torch.float32, device=q.device)
+        out = _empty((geom.n_seqs, geom.n_heads, LATENT_DIM), torch.float32, q.device, stream)
     if workspace is None:
-        workspace = torch.empty(santapp_latent_decode_workspace_bytes(geom, teams, n_sample, cap), dtype=torch.uint8,
-                                device=q.device)
+        workspace = _empty(santapp_latent_decode_workspace_bytes(geom, teams, n_sample, cap), torch.uint8, q.device, stream, False)
     _check(L.santapp_latent_decode_attn(geom.ref(), ctypes.byref(teams.c), _ptr(q), _ptr(suffix_rows),
                                         _ptr(suffix_len), cap, n_sample, int(seed), step, _ptr(step_dev),
                                         stream_base, scale, _ptr(out),
@@ -597,9 +639,9 @@ def santapp_latent_dense_decode_attn(geom: LatentGeometry, teams: LatentTeams, q
     L = load_library()
     cap = 0 if suffix_rows is None else int(suffix_rows.shape[1])
     if out is None:
-        out = torch.empty((geom.n_seqs, geom.n_heads, LATENT_DIM), dtype=torch.float32, device=q.device)
+        out = _empty((geom.n_seqs, geom.n_heads, LATENT_DIM), torch.float32, q.device, stream)
     if workspace is None:
-        workspace = torch.empty(santapp_latent_dense_workspace_bytes(geom, teams), dtype=torch.uint8, device=q.device)
+        workspace = _empty(santapp_latent_dense_workspace_bytes(geom, teams), torch.uint8, q.device, stream, False)
     _check(L.santapp_latent_dense_decode_attn(geom.ref(), ctypes.byref(teams.c), _ptr(q), _ptr(suffix_rows),
                                               _ptr(suffix_len), cap, scale, _ptr(out), _ptr(workspace),
                                               workspace.numel(), _stream_ptr(stream)))
@@ -673,11 +715,11 @@ class Rope:
         return list(self.c.inv_freq[:self.c.rot_dim // 2])
 
 
-def _rope_rows(geom, n, q, k, v, q_out, device):
+def _rope_rows(geom, n, q, k, v, q_out, device, stream):
     d, kv, dt = geom.head_dim, geom.n_kv_heads, geom.torch_dtype
     heads, keys = (n, geom.n_q_heads, d), (n, kv, d)
     if q_out is None:
-        q_out = torch.empty(heads, dtype=dt, device=q.device)
+        q_out = _empty(heads, dt, q.device, stream)
     return (q_out, *_expect_planes("q", q, heads, dt, device), *_expect_planes("k", k, keys, dt, device),
             *_expect_planes("v", v, keys, dt, device), _expect("q_out", q_out, heads, dt, device))
 
@@ -689,7 +731,7 @@ def santapp_rope_append(geom: Geometry, rope: Rope, q: torch.Tensor, k: torch.Te
     """q [B, Hq, d], k and v [B, Hkv, d] (any stride between tokens); base_pos, suffix_len int32 [B]; k_suffix, v_suffix
     [B, Hkv, cap, d]. Row suffix_len[b] is written, q_out returned; suffix_len_out (may be suffix_len) gets suffix_len + 1."""
     B, dt, i32, dev = geom.n_seqs, geom.torch_dtype, torch.int32, _device()
-    q_out, qp, qs, kp, ks, vp, vs, dst = _rope_rows(geom, B, q, k, v, q_out, dev)
+    q_out, qp, qs, kp, ks, vp, vs, dst = _rope_rows(geom, B, q, k, v, q_out, dev, stream)
     cap, one = k_suffix.shape[2], (B,)
     shape = (B, geom.n_kv_heads, cap, geom.head_dim)
     _check(load_library().santapp_rope_append(
@@ -707,7 +749,7 @@ def santapp_rope_prompt(geom: Geometry, rope: Rope, q: torch.Tensor, k: torch.Te
     """q [n, Hq, d], k and v [n, Hkv, d] (any stride between tokens); positions, dst_row int32 [n] or None (the row's
     index); k_prompt, v_prompt [Hkv, rows, d], written at dst_row. Returns q_out [n, Hq, d]."""
     n, dt, i32, dev = q.shape[0], geom.torch_dtype, torch.int32, _device()
-    q_out, qp, qs, kp, ks, vp, vs, dst = _rope_rows(geom, n, q, k, v, q_out, dev)
+    q_out, qp, qs, kp, ks, vp, vs, dst = _rope_rows(geom, n, q, k, v, q_out, dev, stream)
     rows = k_prompt.shape[1]
     shape = (geom.n_kv_heads, rows, geom.head_dim)
     _check(load_library().santapp_rope_prompt(
@@ -767,9 +809,9 @@ def santapp_prefix_decode_attn(geom: Geometry, k_prefix: Optional[torch.Tensor],
         ks = _expect("k_suffix", k_suffix, (B, kv, suffix_cap, d), dt, dev)
         vs = _expect("v_suffix", v_suffix, (B, kv, suffix_cap, d), dt, dev)
     if out is None:
-        out = torch.empty(heads, dtype=torch.float32, device=q.device)
+        out = _empty(heads, torch.float32, q.device, stream)
     if workspace is None:
-        workspace = torch.empty(santapp_prefix_decode_workspace_bytes(geom, n, suffix_cap), dtype=torch.uint8, device=q.device)
+        workspace = _empty(santapp_prefix_decode_workspace_bytes(geom, n, suffix_cap), torch.uint8, q.device, stream, False)
     size = workspace.numel()
     o = _attn_opts(geom, scale, cap, slopes, status, dev)
     _check(load_library().santapp_prefix_decode_attn(
@@ -792,7 +834,7 @@ def santapp_prompt_attn(geom: Geometry, prompt_len, q: torch.Tensor, k_prompt: t
     heads, keys = (sum(prompt_len if new_len is None else new_len), geom.n_q_heads, geom.head_dim), \
         (geom.n_kv_heads, sum(prompt_len), geom.head_dim)
     if out is None:
-        out = torch.empty(heads, dtype=dt, device=q.device)
+        out = _empty(heads, dt, q.device, stream)
     if heads[0] == 0:
         return out
     o = _attn_opts(geom, scale, cap, slopes, status, dev)
