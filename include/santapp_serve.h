@@ -36,7 +36,8 @@ extern "C" {
 typedef struct santapp_rope {
     int32_t rot_dim;           /* rotated values of a head: a multiple of 16, 16..128               */
     int32_t interleaved;       /* 0: pair i is (i, i + rot_dim / 2); 1: (2 i, 2 i + 1)              */
-    double amplitude;          /* 1, or what a long-context scaling multiplies the rotation by      */
+    double amplitude;          /* 1, or what a long-context scaling multiplies the rotation by
+                                  (finite in fp32)                                                  */
     double inv_freq[64];       /* radians per position of pairs 0 .. rot_dim / 2 - 1 (at most 1e6)  */
 } santapp_rope;
 
@@ -103,7 +104,8 @@ int santapp_suffix_fork(const santapp_geom *geom, const int32_t *src, const int3
                         void *v_suffix, int32_t suffix_cap, int32_t *suffix_len_out, santapp_stream stream);
 
 /* How a query scores a key (host struct): s = q.k * scale; with cap > 0, cap * tanh(s / cap); with
- * slopes, less slopes[h] * |position of the query - position of the key|. */
+ * slopes, less slopes[h] * |position of the query - position of the key|. scale and cap times log2 e
+ * have to be finite in fp32, scale / cap a normal number of it (SANTAPP_ERR_INVALID_ARG otherwise). */
 typedef struct santapp_attn_opts {
     float scale;               /* 0: 1 / sqrt(d)                                                    */
     float cap;                 /* 0: none; else > 0                                                 */

@@ -459,8 +459,9 @@ int ta_score(const santapp_attn_opts *opts, TaScore *score)
     const double scale = given == 0.f ? 1.0 / sqrt((double)kHeadDim) : (double)given, log2e = 1.4426950408889634;
     score->scale_log2 = (float)(scale * log2e);
     score->cap_in = cap > 0.f ? (float)(scale / cap) : 0.f;
-    if (isinf(score->cap_in)) return SANTAPP_ERR_INVALID_ARG;
     score->cap_log2 = (float)(cap * log2e);
+    // (0 times an infinite factor would be no number, and a subnormal quotient has lost its lower bits)
+    if (isinf(score->scale_log2) || isinf(score->cap_log2) || (cap > 0.f && !isnormal(score->cap_in))) return SANTAPP_ERR_INVALID_ARG;
     score->slopes = opts ? opts->slopes : nullptr;
     score->status = opts ? opts->status : nullptr;
     return SANTAPP_OK;

@@ -166,7 +166,7 @@ int check_rope(const santapp_geom *geom, const santapp_rope *r, const void *cons
     if (rc != SANTAPP_OK) return rc;
     if (!r) return SANTAPP_ERR_INVALID_ARG;
     if (r->interleaved != 0 && r->interleaved != 1) return SANTAPP_ERR_INVALID_ARG;
-    if (r->rot_dim < 2 || r->rot_dim > kHeadDim || !isfinite(r->amplitude)) return SANTAPP_ERR_INVALID_ARG;
+    if (r->rot_dim < 2 || r->rot_dim > kHeadDim || !isfinite((float)r->amplitude)) return SANTAPP_ERR_INVALID_ARG;
     if (r->rot_dim % 16 != 0) return SANTAPP_ERR_UNSUPPORTED;
     for (int i = 0; i < r->rot_dim / 2; ++i)
         if (!isfinite(r->inv_freq[i]) || fabs(r->inv_freq[i]) > 1e6) return SANTAPP_ERR_INVALID_ARG;
