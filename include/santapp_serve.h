@@ -149,7 +149,8 @@ int santapp_prefix_decode_attn(const santapp_geom *geom, const void *k_prefix, c
  *   prompt_len_host   host int32 [n_seqs], each >= 1
  *   new_len_host      host int32 [n_seqs], 0..prompt_len[b], or NULL: all rows
  *   prefix_len_host   host int32 [n_seqs], 0..prompt_len[b], or NULL: 0
- *   q                 device [sum new_len][n_q_heads][d], sequences one after the other
+ *   q                 device [sum new_len][n_q_heads][d], sequences one after the other (q and out may
+ *                     be NULL where that is no row: nothing is launched then)
  *   k_prompt,v_prompt device [n_kv_heads][sum prompt_len][d]: the layout of santapp_build_teams
  *   out               device [sum new_len][n_q_heads][d] of the element type: it feeds a 16-bit
  *                     product. Sums and softmax statistics are fp32; the weights are rounded to the

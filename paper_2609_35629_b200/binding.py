@@ -833,10 +833,10 @@ def santapp_prompt_attn(geom: Geometry, prompt_len, q: torch.Tensor, k_prompt: t
     dt, dev = geom.torch_dtype, _device()
     heads, keys = (sum(prompt_len if new_len is None else new_len), geom.n_q_heads, geom.head_dim), \
         (geom.n_kv_heads, sum(prompt_len), geom.head_dim)
+    if heads[0] < 0 or keys[1] < 0:
+        _refuse("prompt_len and new_len hold no negative lengths")
     if out is None:
         out = _empty(heads, dt, q.device, stream)
-    if heads[0] == 0:
-        return out
     o = _attn_opts(geom, scale, cap, slopes, status, dev)
     _check(load_library().santapp_prompt_attn(
         geom.ref(), _i32_array(prompt_len), None if new_len is None else _i32_array(new_len),

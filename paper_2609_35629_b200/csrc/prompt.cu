@@ -134,7 +134,7 @@ extern "C" int santapp_prompt_attn(const santapp_geom *geom, const int32_t *prom
     if (rc != SANTAPP_OK) return rc;
     TaScore score;
     if ((rc = ta_score(opts, &score)) != SANTAPP_OK) return rc;
-    if (!prompt_len_host || !q || !k_prompt || !v_prompt || !out) return SANTAPP_ERR_INVALID_ARG;
+    if (!prompt_len_host || !k_prompt || !v_prompt) return SANTAPP_ERR_INVALID_ARG;
     if (misaligned(q, 16) || misaligned(k_prompt, 16) || misaligned(v_prompt, 16) || misaligned(out, 16)) return SANTAPP_ERR_INVALID_ARG;
     const int B = geom->n_seqs, group = geom->n_q_heads / geom->n_kv_heads;
     int64_t keys = 0, tokens = 0;
@@ -144,6 +144,7 @@ extern "C" int santapp_prompt_attn(const santapp_geom *geom, const int32_t *prom
         keys += n;
         tokens += m;
     }
+    if (tokens > 0 && (!q || !out)) return SANTAPP_ERR_INVALID_ARG;
     if (keys >= (int64_t)1 << 30 || tokens * group >= (int64_t)1 << 29) return SANTAPP_ERR_UNSUPPORTED;
     if ((tokens * group / kTaTile + B) * geom->n_kv_heads >= (int64_t)1 << 31) return SANTAPP_ERR_UNSUPPORTED;
     begin_call();
