@@ -155,8 +155,9 @@ int santapp_prefix_decode_attn(const santapp_geom *geom, const void *k_prefix, c
  *   out               device [sum new_len][n_q_heads][d] of the element type: it feeds a 16-bit
  *                     product. Sums and softmax statistics are fp32; the weights are rounded to the
  *                     element type for their product with V (half a step each), the result once
- * A value that is not finite in row i of V also reaches queries of the same sequence up to 127 rows
- * before it; other sequences' rows and memory behind the last row reach nothing.
+ * A value that is not finite in row i of V also reaches queries of the same sequence that see no further
+ * than up to 254 rows before row i (127 where all rows are queries and none is bidirectional); other
+ * sequences' rows and memory behind the last row reach nothing.
  */
 int santapp_prompt_attn(const santapp_geom *geom, const int32_t *prompt_len_host, const int32_t *new_len_host,
                         const int32_t *prefix_len_host, const void *q, const void *k_prompt, const void *v_prompt,

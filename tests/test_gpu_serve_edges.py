@@ -35,3 +35,18 @@ def test_a_fork_on_a_given_stream():
     s.synchronize()
     assert new.tolist() == [3, 20]
     assert torch.equal(k[1], k0[0]) and torch.equal(v[1], v0[0]) and torch.equal(k[0, :, :3], k0[1, :, :3]) and torch.equal(k[0, :, 3:], k0[0, :, 3:])
+
+
+@pytest.mark.parametrize("new,both,hq,hkv", [(None, 0, 1, 1), (None, 0, 28, 4), (257, 0, 1, 1), (130, 0, 7, 1), (None, 300, 1, 1), (400, 461, 16, 2)])
+def test_how_far_an_infinite_value_reaches(new, both, hq, hkv):
+    """Queries that see row i have no finite output; those whose last visible row is more than 254 rows before it are as if it were finite."""
+    n, i = 514, 511
+    m = n if new is None else new
+    geom, q, k, v = sp.Geometry(1, hq, hkv), rand(m, hq, D), rand(hkv, n, D, seed=1), rand(hkv, n, D, seed=2)
+    opts = dict(new_len=None if new is None else [new], prefix_len=[both])
+    want = sp.santapp_prompt_attn(geom, [n], q, k, v, **opts)
+    v[:, i] = float("inf")
+    got = sp.santapp_prompt_attn(geom, [n], q, k, v, **opts)
+    last = torch.maximum(torch.arange(n - m, n, device="cuda"), torch.tensor(both - 1, device="cuda"))
+    assert not bool(torch.isfinite(got[last >= i]).any())
+    assert torch.equal(got[last < i - 254], want[last < i - 254])
