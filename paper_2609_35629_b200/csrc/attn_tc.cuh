@@ -306,7 +306,7 @@ __device__ __forceinline__ void ta_cap_poly(const TaScore &sc, float (&v)[kCols]
 // e = exp(-2 |y|), two uses of the special-function unit, good to 2^-21 there. (Below, it cancels: 2^-22 of the cap would be left of small
 // scores that stand beside large ones.)
 template <int kN>
-__device__ __forceinline__ void ta_cap_far(const TaScore &sc, float (&v)[32])
+__device__ __forceinline__ void ta_cap_far(const TaScore &sc, float (&v)[16])
 {
     static_assert(kN == 4 || kN == 5, "a row of the table");
     const uint64_t in = ta_two(sc.cap_in, sc.cap_in);
@@ -314,7 +314,7 @@ __device__ __forceinline__ void ta_cap_far(const TaScore &sc, float (&v)[32])
 #pragma unroll
     for (int k = 0; k < kN; ++k) c[k] = ta_two(ta_tanh_term<kN>(k) * sc.cap_log2, ta_tanh_term<kN>(k) * sc.cap_log2);
 #pragma unroll
-    for (int i = 0; i < 32; i += 2) {
+    for (int i = 0; i < 16; i += 2) {
         const uint64_t y = ta_mul2(ta_two(v[i], v[i + 1]), in), u = ta_mul2(y, y);
         uint64_t r = c[kN - 1];
 #pragma unroll
@@ -329,8 +329,8 @@ __device__ __forceinline__ void ta_cap_far(const TaScore &sc, float (&v)[32])
         }
     }
 }
-// By a polynomial where the warp's |x cap_in| are at most 1, the usual case. Otherwise 32 of the thread's columns (from t_v on in tensor memory) at a time,
-// there and back, which keeps that path's code short: unrolled over all of them it cost the others 3 to 10 %.
+// By a polynomial where the warp's |x cap_in| are at most 1, the usual case. Otherwise 16 of the thread's columns (from t_v on in tensor memory) at a time,
+// there and back, which keeps that path's code short: unrolled over all of them it cost the others 3 to 10 %, 32 at a time one of them 2 %.
 template <bool kTwo, int kCols>
 __device__ __forceinline__ void ta_cap(const TaScore &sc, uint32_t t_v, float (&v)[kCols])
 {
@@ -347,13 +347,11 @@ __device__ __forceinline__ void ta_cap(const TaScore &sc, uint32_t t_v, float (&
         ta_cap_poly<true, kTwo ? 7 : 6>(sc, v);
     } else {
 #pragma unroll 1
-        for (int q = 0; q < kCols / 32; ++q) {
-            float w[32];
-            ta_ld32(t_v + 32 * q, w);
-            ta_ld_wait();
-            ta_tie(w);
+        for (int q = 0; q < kCols / 16; ++q) {
+            float w[16];
+            ta_ld16(t_v + 16 * q, w);
             ta_cap_far<kTwo ? 5 : 4>(sc, w);
-            ta_st32(t_v + 32 * q, w);
+            ta_st16(t_v + 16 * q, reinterpret_cast<const uint32_t *>(w));
         }
         ta_st_wait();
 #pragma unroll
