@@ -63,7 +63,8 @@ int santapp_rope_frequencies(santapp_rope *rope, double theta, double factor, do
  *   q_out             device [n_seqs][n_q_heads][d], out; may be q itself when q_stride = n_q_heads * d
  *   k_suffix,v_suffix device [n_seqs][n_kv_heads][suffix_cap][d], one row per head written
  *   suffix_len_out    device int32 [n_seqs] or NULL, out: suffix_len + 1; may be suffix_len itself
- *                     (of several layers that share the lengths, the last one's call advances them)
+ *                     (of several layers that share the lengths, the last one's call advances them),
+ *                     must not overlap it otherwise, nor base_pos (refused)
  * A sequence whose suffix is full (suffix_len >= suffix_cap) or whose length is negative (a padded
  * slot) is left alone: nothing of it is written, its length is passed on as it is.
  */

@@ -252,6 +252,13 @@ int santapp_rope_append(const santapp_geom *geom, const santapp_rope *rope, cons
     if (!base_pos || !suffix_len || suffix_cap < 1) return SANTAPP_ERR_INVALID_ARG;
     if (misaligned(base_pos, 4) || misaligned(suffix_len, 4) || misaligned(suffix_len_out, 4)) return SANTAPP_ERR_INVALID_ARG;
     if ((int64_t)geom->n_seqs * geom->n_kv_heads * (int64_t)suffix_cap >= (int64_t)1 << 31) return SANTAPP_ERR_UNSUPPORTED;
+    if (suffix_len_out) {                                       // other blocks still read lengths and positions when one writes its new length
+        const uintptr_t bytes = sizeof(int32_t) * (uintptr_t)geom->n_seqs, o = reinterpret_cast<uintptr_t>(suffix_len_out);
+        for (const int32_t *in : {base_pos, suffix_len}) {
+            const uintptr_t i = reinterpret_cast<uintptr_t>(in);
+            if (o < i + bytes && i < o + bytes && !(in == suffix_len && o == i)) return SANTAPP_ERR_INVALID_ARG;
+        }
+    }
     RopeParams p = rope_params(q, q_stride, k, k_stride, v, v_stride, q_out, k_suffix, v_suffix);
     p.n_rows = geom->n_seqs;
     p.positions = base_pos;

@@ -59,3 +59,9 @@ def test_scales_and_caps_that_fp32_cannot_hold_are_refused(lib, scale, cap, want
 def test_an_amplitude_beyond_fp32_is_refused(lib):
     r = sp.CRope(128, 0, 1e39, (ctypes.c_double * 64)(*([0.5] * 64)))
     assert lib.santapp_rope_append(geom(), ctypes.byref(r), A, 28 * 128, A, 512, A, 512, A, A, A, A, A, 16, None, None) == BAD
+
+
+@pytest.mark.parametrize("new", [0x30000 + 4, 0x30000 - 4, 0x40000, 0x40000 + 4])
+def test_append_refuses_lengths_that_overlap_what_it_reads(lib, new):
+    r = sp.CRope(128, 0, 1.0, (ctypes.c_double * 64)(*([0.5] * 64)))
+    assert lib.santapp_rope_append(geom(), ctypes.byref(r), A, 28 * 128, A, 512, A, 512, 0x40000, 0x30000, A, A, A, 16, new, None) == BAD
