@@ -105,7 +105,9 @@ int santapp_suffix_fork(const santapp_geom *geom, const int32_t *src, const int3
                         void *v_suffix, int32_t suffix_cap, int32_t *suffix_len_out, santapp_stream stream);
 
 /* How a query scores a key (host struct): s = q.k * scale; with cap > 0, cap * tanh(s / cap); with
- * slopes, less slopes[h] * |position of the query - position of the key|. scale and cap times log2 e
+ * slopes, less slopes[h] * |position of the query - position of the key|. Both attention calls let a
+ * weight grow to 2^24 before its sums are rescaled (bf16; fp16 keeps to its own range), so values of V
+ * above 2^80 may overflow on the way. scale and cap times log2 e
  * have to be finite in fp32, scale / cap a normal number of it (SANTAPP_ERR_INVALID_ARG otherwise). */
 typedef struct santapp_attn_opts {
     float scale;               /* 0: 1 / sqrt(d)                                                    */
@@ -120,7 +122,9 @@ typedef struct santapp_attn_opts {
  * One decode step of a batch whose sequences share one prompt (several answers to it, or questions
  * about it): query heads of sequence b attend all prefix rows and the suffix_len[b] rows of their own
  * suffix; the prompt's rows are read once for the batch, not once per sequence. Equal to
- * santapp_dense_decode_attn on records that repeat the prompt for every sequence.
+ * santapp_dense_decode_attn on records that repeat the prompt for every sequence. The last bits of a
+ * sequence's rows depend on the batch it is in: its size decides how the prompt is cut, and 32 rows that
+ * a warp works on share the moments at which their sums are rescaled and the form of their tanh.
  *   k_prefix,v_prefix device [n_kv_heads] planes of prefix_len rows [d], plane_rows rows apart
  *                     (plane_rows >= prefix_len): a prompt in token order, or k_packed / v_packed of
  *                     records built for one sequence (attention does not depend on row order)
@@ -155,7 +159,9 @@ int santapp_prefix_decode_attn(const santapp_geom *geom, const void *k_prefix, c
  *   k_prompt,v_prompt device [n_kv_heads][sum prompt_len][d]: the layout of santapp_build_teams
  *   out               device [sum new_len][n_q_heads][d] of the element type: it feeds a 16-bit
  *                     product. Sums and softmax statistics are fp32; the weights are rounded to the
- *                     element type for their product with V (half a step each), the result once
+ *                     element type for their product with V (half a step each), the result once.
+ *                     The tensor core cuts its sums to fp32 instead of rounding them, which shows
+ *                     where very many keys weigh alike: 0.04 % too little at 2^20 keys, 2.4 % at 2^23
  * A value that is not finite in row i of V also reaches queries of the same sequence that see no further
  * than up to 254 rows before row i (127 where all rows are queries and none is bidirectional); other
  * sequences' rows and memory behind the last row reach nothing.

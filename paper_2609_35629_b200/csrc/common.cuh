@@ -194,9 +194,11 @@ inline cudaError_t ensure_dynamic_smem(const void *fn, int bytes, std::atomic<un
 // running (programmatic stream serialisation), and starts with step_wait(), which returns once that
 // kernel has completed. Outside a CUDA graph a plain launch behind a running kernel cost 1.5 us more than
 // inside one; with this the eager step takes what the graph takes (28 layers of batch 1 at 32K: 903 ->
-// 712 us, dense 587 -> 484) and the graph gains 1 to 5 %. No kernel asks for its successor early
+// 712 us, dense 587 -> 484) and the graph gains 1 to 5 %. Kernels do not ask for their successor early
 // (griddepcontrol.launch_dependents): blocks that are resident before their inputs are ready were in the way of
-// the blocks still to run (747 us with it in every kernel, 728 with it in the scorer and the merge alone).
+// the blocks still to run (747 us with it in every kernel, 728 with it in the scorer and the merge alone). The one exception is
+// the pair of a call in prefix.cu: prefix_kernel asks, each block behind its own step_wait(), so everything before the pair on the stream
+// has completed when finish_kernel's blocks begin; those read what the pair does not write, and wait before anything else.
 template <typename... KArgs, typename... Args>
 inline cudaError_t launch_step(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t s, Args... args)
 {
@@ -469,7 +471,8 @@ __device__ __forceinline__ uint32_t pick_word(const uint4 &w, int i)
 
 // First statement of every kernel that launch_step launches, in every thread, ahead of any access to global
 // memory and of any early return: a block that left without it would let the kernel after this one
-// start before the kernel before this one has finished.
+// start before the kernel before this one has finished. (finish_kernel of prefix.cu reads first what its predecessor cannot
+// write, and waits, in every thread, before it writes anything.)
 __device__ __forceinline__ void step_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
 // Diagnostic: thread 0 of a block notes the device timer (ns) in slot `slot` of its block's marks.

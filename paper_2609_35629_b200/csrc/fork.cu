@@ -6,7 +6,7 @@
 // block touches these rows, so one launch does it without a second buffer.
 //
 // Bound by memory: each moved row is read and written once. Rows of slots that stay are not touched: the block's threads go through a list of
-// the slots that move. 16 of 32 slots of up to 1024 rows (26.5 MB, 4.1 us at the copy rate) take 7.5 us.
+// the slots that move. 16 of 32 slots of up to 1024 rows (26.5 MB, 4.1 us at the copy rate) take 7.4 us.
 #include "common.cuh"
 #include "santapp_serve.h"
 
@@ -16,7 +16,7 @@ namespace {
 
 constexpr int kForkThreads = 256;
 // Bytes of rows a block stages at most, while one row of every slot is no more: a block waits for memory twice (its table, its rows), so
-// what hides that is blocks beside it, six of this size an SM (that case: 7.7 us; 16, 24 and 64 KB 9.1, 9.0 and 8.2)
+// what hides that is blocks beside it, six of this size an SM (that case, when these were compared: 7.7 us; 16, 24 and 64 KB 9.1, 9.0 and 8.2)
 constexpr int kForkStage = 32 * 1024;
 constexpr int kForkMaxSeqs = 4096;
 

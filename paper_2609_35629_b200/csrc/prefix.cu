@@ -8,7 +8,7 @@
 //
 // Up to 128 rows (18 sequences of 7 heads) the prompt's bytes bound the first kernel, 512 per row and KV head: 5 sequences of 32 heads over
 // 131071 rows, 541 MB, take 93 us in it (5.8 TB/s, 0.90 of the copy rate). Beyond, its products and weights: 4 d per row and key, half again
-// for the weights' second term (the outputs are fp32); 64 sequences of 28 heads over 32768 rows with a cap, 73 us, the tensor core busy 41 %.
+// for the weights' second term (the outputs are fp32); 64 sequences of 28 heads over 32768 rows with a cap, 68 us, the tensor core busy 43 %.
 // The merge: 3 us for a pair's suffix and 2 for its partials, another 2 where a cluster shares it (two cluster barriers).
 #include <algorithm>
 #include <math.h>

@@ -2,8 +2,8 @@
 //
 // A block takes 256 query rows (a KV head's query heads of 256 / group tokens) of one sequence and every key tile that one of them sees:
 // 4 d operations per query head and visible pair, far more than the bytes, so tensor cores and exponentials bound
-// it: 8192 rows of 28 heads over 4 KV heads, 0.48 PFLOP, take 390 us (1.23 PFLOP/s, 0.74 of the library product's burst rate; tensor core
-// busy 59 %, special-function unit 59 %, the card at its power limit when it is repeated). Blocks run from the longest sequence's last rows (which see most keys) down, so that the last ones are short. Where 256 rows a
+// it: 8192 rows of 28 heads over 4 KV heads, 0.48 TFLOP, take 380 to 450 us inside a graph (1.07 to 1.27 PFLOP/s, 0.64 to 0.76 of the library
+// product's burst rate; tensor core busy 59 %, special-function unit 59 %, the card at its power limit when it is repeated). Blocks run from the longest sequence's last rows (which see most keys) down, so that the last ones are short. Where 256 rows a
 // block leave SMs idle or the longest block alone (item_rows), a block takes 128, whose two streams share the keys.
 // The sequences' tables travel in the kernel's arguments, kPromptSeqs at a launch.
 #include <algorithm>

@@ -19,7 +19,7 @@ namespace {
 
 constexpr int kRopeThreads = 256;
 // Many rows: four tokens a block, two units of 32 bytes a thread under way and six blocks an SM. A 32K prompt's 28 + 4 + 4 heads (604 MB)
-// take 100 us, 6.0 TB/s (93 % of the copy rate); five units and three blocks 117, one token a block 114, eight blocks 99 to 109.
+// take 100 us inside a graph, 6.0 TB/s (93 % of the copy rate), 109 eagerly; five units and three blocks 117, one token a block 114, eight blocks 99 to 109.
 constexpr int kMany = 4, kManyAhead = 2, kManyBlocks = 6;
 constexpr int kUnits = 8;                 // units of a head: two 16-byte pieces that hold both values of eight pairs
 
