@@ -36,6 +36,10 @@ namespace santapp {
 
 constexpr int kTaThreads = 384;           // warps 0-3, 4-7: a row per thread of streams 0, 1; warp 8: copies; warp 9: products; warp 10: the
                                           // last tile's values that are somebody else's; warp 11: its keys, where scores are capped
+// Registers a thread at launch, at most what kTaThreads leave each (and what the compiler gives them), and after the split: the softmax warps take
+// what the other four leave.
+constexpr int kTaRegs = 168, kTaRegsSoftmax = 192, kTaRegsOther = 120;
+static_assert(8 * kTaRegsSoftmax + 4 * kTaRegsOther <= 12 * kTaRegs, "the split draws on the registers at launch");
 constexpr int kTaTile = 128;              // query rows of a stream, keys of a tile
 constexpr int kTaTileBytes = kTaTile * kHeadDim * 2;
 constexpr int kTaRing = 5;                // tiles of keys or values under way
@@ -565,9 +569,8 @@ __device__ __forceinline__ void ta_block(TaSmem &sm, const TaItem &it, const TaS
     __syncthreads();
     tc_fence_after();
 
-    // registers: 168 a thread at launch; the softmax warps take what the other four leave (8 * 192 + 4 * 120 = 12 * 168)
     if (warp < 8) {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kTaRegsSoftmax));
         // ---- a row of scores per thread ----
         asm volatile("cp.async.wait_all;" ::: "memory");
         proxy_fence();
@@ -582,7 +585,7 @@ __device__ __forceinline__ void ta_block(TaSmem &sm, const TaItem &it, const TaS
         const bool ok = ta_softmax<kHalf, kTwo, kCap, kBias, kCols>(sm, it, sc, s, live, vis, q_pos, slope, key_pos, m, l);
         finish(ok, s, live, m, l);
     } else {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 120;");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kTaRegsOther));
         if (warp == 8) {
             // ---- copies ----
             if (ta_elect()) {
@@ -830,5 +833,19 @@ __device__ __forceinline__ void ta_rows(TaSmem &sm, const TaItem &it, bool ok, i
 // rows behind `rows` read as zeros. Returns false where the driver refuses.
 bool ta_tensor_map(CUtensorMap *map, const void *base, int64_t rows, int64_t plane_rows, int n_planes, bool half);
 int ta_score(const santapp_attn_opts *opts, TaScore *score);     // a santapp_status
+// What a kernel on this file needs once per device. One that was built with fewer registers than its split asks for would wait for them for
+// ever: it is not launched.
+inline cudaError_t ta_prepare(const void *kernel, std::atomic<unsigned long long> &done)
+{
+    int dev = 0;
+    cudaError_t err = cudaGetDevice(&dev);
+    if (err != cudaSuccess) return err;
+    if (dev >= 64 || !(done.load(std::memory_order_acquire) >> dev & 1)) {
+        cudaFuncAttributes a;
+        if ((err = cudaFuncGetAttributes(&a, kernel)) != cudaSuccess) return err;
+        if (a.numRegs < kTaRegs) return cudaErrorInvalidKernelImage;
+    }
+    return ensure_dynamic_smem(kernel, kTaSmemBytes, done);
+}
 
 }  // namespace santapp

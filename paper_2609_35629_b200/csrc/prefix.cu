@@ -529,7 +529,7 @@ int santapp_prefix_decode_attn(const santapp_geom *geom, const void *k_prefix, c
     else      kernels_of<false>(cap, bias, fold, &prefix, &finish);
     static std::atomic<unsigned long long> opted[4][8];
     const int which = (half ? 4 : 0) + (cap ? 2 : 0) + (bias ? 1 : 0);
-    cudaError_t err = ensure_dynamic_smem(reinterpret_cast<const void *>(prefix), kTaSmemBytes, opted[fold == 4 ? 2 : fold - 1][which]);
+    cudaError_t err = ta_prepare(reinterpret_cast<const void *>(prefix), opted[fold == 4 ? 2 : fold - 1][which]);
     if (err == cudaSuccess) err = ensure_dynamic_smem(reinterpret_cast<const void *>(finish), (int)sizeof(FinishSmem), opted[3][which]);
     if (err != cudaSuccess) return note_cuda_failure(err, "prefix attention set-up");
     int launches = 0;

@@ -167,7 +167,7 @@ extern "C" int santapp_prompt_attn(const santapp_geom *geom, const int32_t *prom
                                                 : prompt_kernel_of<false>(score.cap_log2 > 0.f, score.slopes != nullptr);
     static std::atomic<unsigned long long> opted[8];
     const int which = (geom->elem_type ? 4 : 0) + (score.cap_log2 > 0.f ? 2 : 0) + (score.slopes != nullptr ? 1 : 0);
-    cudaError_t err = ensure_dynamic_smem(reinterpret_cast<const void *>(kernel), kTaSmemBytes, opted[which]);
+    cudaError_t err = ta_prepare(reinterpret_cast<const void *>(kernel), opted[which]);
     if (err != cudaSuccess) return note_cuda_failure(err, "prompt attention set-up");
     int launches = 0, key0 = 0, token0 = 0;
     for (int first = 0; first < B;) {
