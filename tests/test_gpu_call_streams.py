@@ -105,3 +105,23 @@ def test_an_output_may_be_used_and_dropped_on_the_current_stream():
             torch.full(tuple(want.shape), float("nan"), device="cuda")
     torch.cuda.synchronize()
     assert all(torch.equal(x, want) for x in kept)
+
+
+def test_a_captured_call_on_a_stream_of_its_own():
+    """A branch of a captured graph that makes its own buffers: they are the graph's, and stay so."""
+    call, size = cases()["prefix_decode"]
+    want = call(None)
+    s = torch.cuda.Stream()
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        s.wait_stream(torch.cuda.current_stream())
+        got = [call(s) for _ in range(2)]
+        torch.cuda.current_stream().wait_stream(s)
+        both = got[0] + got[1]
+    other = [torch.full((size,), 85, dtype=torch.uint8, device="cuda") for _ in range(3)]
+    for _ in range(3):
+        graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(got[0], want) and torch.equal(got[1], want) and torch.equal(both, want + want)
+    assert all(bool((x == 85).all()) for x in other)
